@@ -326,6 +326,87 @@ int sfb_dual_to_primal_l2(sfb_ctx* ctx, const float* Z, float* W, int64_t J, int
  */
 int sfb_prox_rows(sfb_ctx* ctx, float* W, int64_t J, int64_t D, int32_t mode);
 
+/*
+ * Factor blocks beside a shared matrix: low-rank adapters of many requests.  A factor block that is NOT applied to W but
+ * kept beside it changes the model for the requests that use it alone: block a stands for
+ *       W + scale[a] * sum_{r < ranks[a]} U_a[r] V_a[r]^T
+ * (what sfb_apply(W, U_a, V_a, ranks[a], -scale[a]) would make of W), U_a [rank][J], V_a [rank][D]: the layout in which
+ * factors are buffered and sent.  A pool of `count` blocks of equal room is one array each of U [count][rank][J] and
+ * V [count][rank][D]; pairs from ranks[a] on are not used (what lies there does not matter, not-a-numbers included).
+ *
+ * The rows of a batch are packed: request q is the rows start[q] .. start[q + 1] - 1 of X (any length from zero on) and
+ * uses block adapter[q]; a number outside [0, count) means none, the shared matrix alone.  Rows in front of start[0] and
+ * from start[requests] on belong to no request: they are not computed, and the outputs' rows there stay as they were (a
+ * padded batch).  start and adapter are device arrays, read when the call runs, so that a captured graph serves batches of
+ * other compositions; start must be non-decreasing in [0, T] (other values give unspecified results in the rows they touch,
+ * nothing is read or written out of bounds).
+ */
+typedef struct {
+    const void* U;         /* [count][rank][J] of dtype */
+    const void* V;         /* [count][rank][D] of dtype */
+    const int32_t* ranks;  /* [count] device; pairs in use, clamped to [0, rank]; NULL: all */
+    const float* scale;    /* [count] device; NULL: 1 */
+    int64_t count;         /* 0: no blocks (U and V are not looked at), up to 65536 */
+    int32_t rank;          /* 1 .. SFB_ADAPTER_MAX_RANK; without blocks also 0 */
+    int32_t dtype;         /* sfb_dtype of U, V and of the rows */
+} sfb_adapters;
+#define SFB_ADAPTER_MAX_RANK 256
+
+typedef struct {
+    const int64_t* start;   /* [count + 1] device */
+    const int32_t* adapter; /* [count] device */
+    int64_t count;          /* requests, >= 0 */
+} sfb_requests;
+
+/*
+ * sfb_adapter_forward: for every row t of a request, with its block a,
+ *       H[t][r] = scale[a] * sum_d X[t][d] V_a[r][d]
+ *       Y[t][j] = sum_d X[t][d] W[j][d] + sum_{r < ranks[a]} H[t][r] U_a[r][j].
+ * X [T][D], Y [T][J] of the blocks' dtype; sums in fp32.  H (may be NULL) receives the projections [T][rank] in fp32 (zeros
+ * for r >= ranks[a] and for rows without a block), which the backward pass can use again.
+ * W, fp32 blocks: the fp32 array (w_dtype SFB_F32).  bf16 blocks: a row-major bf16 array [J][D] (w_dtype SFB_BF16), or the
+ * fp32 array that is attached to this context with a bf16 working copy or as two planes (w_dtype SFB_F32): the copy or the
+ * high plane is read.  bf16 needs J % 8 == 0 and D % 8 == 0, and takes J and D up to 4194304.
+ *
+ * sfb_adapter_backward: the gradients of a loss with dY = d loss / d Y given,
+ *       dH[t][r] = scale[a] * sum_j dY[t][j] U_a[r][j]
+ *       dX[t][d] = sum_j dY[t][j] W[j][d] + sum_r dH[t][r] V_a[r][d]
+ *       dU_a[r][j] = sum_{t of a} H[t][r] dY[t][j],   dV_a[r][d] = sum_{t of a} dH[t][r] X[t][d]
+ * dX [T][D] of the blocks' dtype (NULL: not wanted), dU [count][rank][J] and dV [count][rank][D] fp32 (both NULL: not
+ * wanted), overwritten whole: blocks without rows and pairs that are not in use get zeros.  H: what the forward pass gave, or
+ * NULL (computed again).  The gradient of W itself is the factor pair (dY, X): sfb_apply takes it as it is.
+ * Rows of no request contribute nothing, whatever they hold.  Every sum is made in a fixed order: equal calls give equal bits.
+ * Outputs must not overlap inputs.  The workspace queries give the bytes either call needs for up to T rows; the workspace
+ * holds nothing between calls.
+ */
+int64_t sfb_adapter_forward_workspace_bytes(int64_t J, int64_t D, int64_t T, const sfb_adapters* adapters);
+int sfb_adapter_forward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J, int64_t D, const void* X, int64_t T,
+                        const sfb_adapters* adapters, const sfb_requests* requests, void* Y, float* H);
+int64_t sfb_adapter_backward_workspace_bytes(int64_t J, int64_t D, int64_t T, const sfb_adapters* adapters);
+int sfb_adapter_backward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J, int64_t D, const void* X, const void* dY,
+                         int64_t T, const sfb_adapters* adapters, const sfb_requests* requests, const float* H, void* dX,
+                         float* dU, float* dV);
+
+/*
+ * The global norm of the gradients of a step, and their clipping.  The gradients are a list of tensors (host array; device
+ * pointers, aligned to their elements, 16 bytes for full speed), fp32 and bf16 mixed:
+ *       norm = sqrt(sum_i sum_k g_i[k]^2),      dst_i[k] = src_i[k] * min(1, max_norm / norm).
+ * sfb_grad_norm writes *norm (device); it does not look at dst.  sfb_clip_grads does both; dst_i may be src_i (scaled in
+ * place, and left alone where the norm is within the bound) or another tensor (always written), otherwise tensors must not
+ * overlap.  Squares are summed in 64 bits in a fixed order.  max_norm >= 0.  A norm that is not finite is reported as it is,
+ * and the scale is then 0 (infinite) or not a number: look at *norm before the gradients are used.
+ * Needs the workspace of sfb_grad_norm_workspace_bytes.
+ */
+typedef struct {
+    const void* src;   /* [n] of dtype */
+    void* dst;         /* [n] of dtype; sfb_clip_grads only */
+    int64_t n;         /* elements, >= 0 */
+    int32_t dtype;     /* sfb_dtype */
+} sfb_tensor;
+int64_t sfb_grad_norm_workspace_bytes(const sfb_tensor* list, int64_t count);
+int sfb_grad_norm(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, float* norm);
+int sfb_clip_grads(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, float max_norm, float* norm);
+
 /* Static description of a status code. */
 const char* sfb_strerror(int code);
 /* hipError_t (as int) of the last failed HIP call on this context, 0 if none. */

@@ -48,6 +48,26 @@ class sfb_csr(ctypes.Structure):
     ]
 
 
+class sfb_adapters(ctypes.Structure):
+    _fields_ = [
+        ("U", ctypes.c_void_p),
+        ("V", ctypes.c_void_p),
+        ("ranks", ctypes.c_void_p),
+        ("scale", ctypes.c_void_p),
+        ("count", ctypes.c_int64),
+        ("rank", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+    ]
+
+
+class sfb_requests(ctypes.Structure):
+    _fields_ = [("start", ctypes.c_void_p), ("adapter", ctypes.c_void_p), ("count", ctypes.c_int64)]
+
+
+class sfb_tensor(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
 class sfb_kernel_time(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char_p), ("launches", ctypes.c_int32), ("total_ms", ctypes.c_float)]
 
@@ -124,6 +144,20 @@ def lib():
         L.sfb_sdca_mlr_sf.restype = ctypes.c_int
         L.sfb_dual_to_primal_l2.argtypes = [vp, vp, vp, i64, i64, ctypes.c_float]
         L.sfb_dual_to_primal_l2.restype = ctypes.c_int
+        pa, pr, pt = ctypes.POINTER(sfb_adapters), ctypes.POINTER(sfb_requests), ctypes.POINTER(sfb_tensor)
+        for name in ("sfb_adapter_forward_workspace_bytes", "sfb_adapter_backward_workspace_bytes"):
+            getattr(L, name).argtypes = [i64, i64, i64, pa]
+            getattr(L, name).restype = i64
+        L.sfb_adapter_forward.argtypes = [vp, vp, i32, i64, i64, vp, i64, pa, pr, vp, vp]
+        L.sfb_adapter_forward.restype = ctypes.c_int
+        L.sfb_adapter_backward.argtypes = [vp, vp, i32, i64, i64, vp, vp, i64, pa, pr, vp, vp, vp, vp]
+        L.sfb_adapter_backward.restype = ctypes.c_int
+        L.sfb_grad_norm_workspace_bytes.argtypes = [pt, i64]
+        L.sfb_grad_norm_workspace_bytes.restype = i64
+        L.sfb_grad_norm.argtypes = [vp, pt, i64, vp]
+        L.sfb_grad_norm.restype = ctypes.c_int
+        L.sfb_clip_grads.argtypes = [vp, pt, i64, ctypes.c_float, vp]
+        L.sfb_clip_grads.restype = ctypes.c_int
         L.sfb_prox_rows.argtypes = [vp, vp, i64, i64, i32]
         L.sfb_prox_rows.restype = ctypes.c_int
         L.sfb_strerror.argtypes = [ctypes.c_int]
@@ -201,6 +235,34 @@ def _ptr(t, name, dtype=None, shape=None):
     return t.data_ptr()
 
 
+class TensorList:
+    """A list of tensors for sfb_grad_norm and sfb_clip_grads, made once and used for as long as the tensors keep their
+    memory: `src` the gradients (fp32 or bf16, contiguous, any sizes), `dst` where the clipped ones go (None: in place)."""
+
+    def __init__(self, src, dst=None):
+        src = list(src)
+        dst = src if dst is None else list(dst)
+        if len(dst) != len(src):
+            raise ValueError("src and dst must have the same number of tensors")
+        self.tensors = (src, dst)        # (kept alive with the list)
+        self.device = None
+        self.items = (sfb_tensor * max(1, len(src)))()
+        self.count = len(src)
+        for k, (s, d) in enumerate(zip(src, dst)):
+            item = self.items[k]
+            item.src, item.n, item.dtype = _ptr(s, "src[%d]" % k), s.numel(), _dtype_code(s)
+            item.dst = item.src if d is s else _ptr(d, "dst[%d]" % k, dtype=s.dtype, shape=tuple(s.shape))
+            for t in (s, d):
+                if self.device is None:
+                    self.device = t.device
+                elif t.device != self.device:
+                    raise ValueError("the tensors of a list must be on one device")
+        need = lib().sfb_grad_norm_workspace_bytes(self.items, self.count)
+        if need < 0:
+            raise SfbError(int(need), "sfb_grad_norm_workspace_bytes")
+        self.workspace_bytes = int(need)
+
+
 class Context:
     """One sfb_ctx bound to a device and a stream; owns a torch workspace tensor."""
 
@@ -214,6 +276,7 @@ class Context:
         if rc != SFB_OK:
             raise SfbError(rc, "sfb_create")
         self._ws = None
+        self._captured, self._retired = False, []      # workspaces that captured graphs may still work in
         self._shadow = None          # (W tensor, buffer tensor)
 
     # -- bf16 working copy of W ----------------------------------------------
@@ -300,6 +363,8 @@ class Context:
 
     def sfb_set_workspace(self, tensor):
         """Use `tensor` (uint8, device) as scratch; None clears it."""
+        if self._captured and self._ws is not None and self._ws is not tensor:
+            self._retired.append(self._ws)
         if tensor is None:
             self._check(lib().sfb_set_workspace(self._h, None, 0), "sfb_set_workspace")
         else:
@@ -470,6 +535,93 @@ class Context:
         rc = lib().sfb_dual_to_primal_l2(self._h, _ptr(Z, "Z", dtype=torch.float32, shape=(J, D)),
                                          _ptr(W, "W", dtype=torch.float32), J, D, float(lam))
         self._check(rc, "sfb_dual_to_primal_l2")
+
+    # -- factor blocks beside a shared matrix -----------------------------------
+    def _here(self, **tensors):
+        for name, t in tensors.items():
+            if t is not None and t.device != self.device:
+                raise ValueError("%s must be on %s, got %s" % (name, self.device, t.device))
+
+    def _stream_workspace(self, need):
+        """Room for `need` bytes, allocated on the context's stream.  What a captured graph works in stays allocated when the
+        workspace grows: the graph replays on the old one."""
+        capturing = torch.cuda.is_current_stream_capturing()
+        if self._ws is None or need > self._ws.numel():
+            self._captured = self._captured or capturing
+            if self._ws is not None and not self._captured:
+                self._ws.record_stream(self.stream)
+            with torch.cuda.stream(self.stream):
+                self.sfb_set_workspace(torch.empty(need, dtype=torch.uint8, device=self.device))
+        self._captured = self._captured or capturing
+
+    def _adapters(self, W, X, start, adapter, U, V, ranks, scale):
+        J, D = W.shape
+        if U.dim() != 3 or V.dim() != 3 or X.dim() != 2:
+            raise ValueError("U and V must be [count][rank][...], X [T][D]")
+        n, R = U.shape[0], U.shape[1]
+        self._here(W=W, X=X, start=start, adapter=adapter, U=U, V=V, ranks=ranks, scale=scale)
+        ad, rq = sfb_adapters(), sfb_requests()
+        ad.count, ad.rank, ad.dtype = n, R, _dtype_code(X)
+        ad.U = _ptr(U, "U", dtype=X.dtype, shape=(n, R, J))
+        ad.V = _ptr(V, "V", dtype=X.dtype, shape=(n, R, D))
+        ad.ranks = None if ranks is None else _ptr(ranks, "ranks", dtype=torch.int32, shape=(n,))
+        ad.scale = None if scale is None else _ptr(scale, "scale", dtype=torch.float32, shape=(n,))
+        S = adapter.numel()
+        rq.start = _ptr(start, "start", dtype=torch.int64, shape=(S + 1,))
+        rq.adapter = _ptr(adapter, "adapter", dtype=torch.int32, shape=(S,))
+        rq.count = S
+        return J, D, X.shape[0], ad, rq
+
+    def sfb_adapter_forward(self, W, X, start, adapter, U, V, Y, ranks=None, scale=None, H=None):
+        """Enqueues Y = X W^T + H U_a (H = scale_a X V_a^T, written too where a tensor for it is given): rows
+        start[q] .. start[q + 1] - 1 of X [T][D] with the factor block a = adapter[q] of U [n][R][J], V [n][R][D] (outside
+        [0, n): none).  start int64 [S + 1] and adapter int32 [S] on the device; rows of no request stay as they are."""
+        J, D, T, ad, rq = self._adapters(W, X, start, adapter, U, V, ranks, scale)
+        self._here(Y=Y, H=H)
+        need = lib().sfb_adapter_forward_workspace_bytes(J, D, T, ctypes.byref(ad))
+        if need < 0:
+            raise SfbError(int(need), "sfb_adapter_forward_workspace_bytes")
+        self._stream_workspace(int(need))
+        rc = lib().sfb_adapter_forward(self._h, _ptr(W, "W"), _dtype_code(W), J, D, _ptr(X, "X", shape=(T, D)), T, ctypes.byref(ad),
+                                       ctypes.byref(rq), _ptr(Y, "Y", dtype=X.dtype, shape=(T, J)),
+                                       None if H is None else _ptr(H, "H", dtype=torch.float32, shape=(T, ad.rank)))
+        self._check(rc, "sfb_adapter_forward")
+
+    def sfb_adapter_backward(self, W, X, dY, start, adapter, U, V, dX=None, dU=None, dV=None, ranks=None, scale=None, H=None):
+        """Enqueues the gradients of the forward call at dY [T][J]: dX of X's dtype, dU [n][R][J] and dV [n][R][D] fp32
+        (None: not wanted).  H: what the forward call wrote, or None."""
+        J, D, T, ad, rq = self._adapters(W, X, start, adapter, U, V, ranks, scale)
+        self._here(dY=dY, dX=dX, dU=dU, dV=dV, H=H)
+        need = lib().sfb_adapter_backward_workspace_bytes(J, D, T, ctypes.byref(ad))
+        if need < 0:
+            raise SfbError(int(need), "sfb_adapter_backward_workspace_bytes")
+        self._stream_workspace(int(need))
+        n, R = ad.count, ad.rank
+        rc = lib().sfb_adapter_backward(self._h, _ptr(W, "W"), _dtype_code(W), J, D, _ptr(X, "X", shape=(T, D)),
+                                        _ptr(dY, "dY", dtype=X.dtype, shape=(T, J)), T, ctypes.byref(ad), ctypes.byref(rq),
+                                        None if H is None else _ptr(H, "H", dtype=torch.float32, shape=(T, R)),
+                                        None if dX is None else _ptr(dX, "dX", dtype=X.dtype, shape=(T, D)),
+                                        None if dU is None else _ptr(dU, "dU", dtype=torch.float32, shape=(n, R, J)),
+                                        None if dV is None else _ptr(dV, "dV", dtype=torch.float32, shape=(n, R, D)))
+        self._check(rc, "sfb_adapter_backward")
+
+    # -- norm and clipping of gradients ------------------------------------------
+    def _list(self, tensors, norm):
+        if tensors.device is not None and tensors.device != self.device:
+            raise ValueError("the tensors must be on %s, got %s" % (self.device, tensors.device))
+        self._here(norm=norm)
+        self._stream_workspace(tensors.workspace_bytes)
+        return _ptr(norm, "norm", dtype=torch.float32, shape=(1,))
+
+    def sfb_grad_norm(self, tensors: TensorList, norm):
+        """Enqueues norm[0] = the global 2-norm of the list's tensors."""
+        p = self._list(tensors, norm)
+        self._check(lib().sfb_grad_norm(self._h, tensors.items, tensors.count, p), "sfb_grad_norm")
+
+    def sfb_clip_grads(self, tensors: TensorList, max_norm, norm):
+        """Enqueues norm[0] and dst = src * min(1, max_norm / norm) for every tensor of the list."""
+        p = self._list(tensors, norm)
+        self._check(lib().sfb_clip_grads(self._h, tensors.items, tensors.count, float(max_norm), p), "sfb_clip_grads")
 
     def sfb_prox_rows(self, W, mode=SFB_PROX_PROJECT):
         J, D = W.shape

@@ -1,0 +1,93 @@
+// Internal launch interface of the adapter calls (factor blocks beside a shared projection, their gradients) and of the
+// norm and clipping of gradients.  Every function only enqueues work on `stream` and returns the launch status.
+#pragma once
+#include "../../include/sfb.h"
+#include "kernels.h"
+
+namespace sfb {
+
+// Which rows belong to whom: request q is the rows start[q] .. start[q + 1] - 1 and uses factor block adapter[q] of the pool
+// (outside [0, count): none).  Device arrays; the kernels clamp what they read from them.
+struct AdapterRows {
+    const int64_t* start;
+    const int32_t* adapter;
+    int64_t requests;
+    const int32_t* ranks;      // nullable: every block has all `rank` pairs
+    const float* scale;        // nullable: 1
+    int64_t count;             // factor blocks in the pool
+    int rank;                  // pairs a block has room for
+    int64_t T;                 // rows of the buffers
+};
+// Leading dimension of the kernels' own array of projections: `rank` rounded up to whole MFMA tiles.
+__host__ __device__ inline int adapter_pitch(int rank) { return (rank + 15) / 16 * 16; }
+constexpr int ROW_NONE = -1, ROW_OUTSIDE = -2;      // row_adapter: a request without a block; no request at all
+
+// H[t][r] = scale_a sum_k X[t][k] F_a[r][k], F [count][rank][K] of X's type; zeros for r >= ranks[a] and for rows without a
+// block.  row_adapter[t] (written): the block of row t, ROW_NONE or ROW_OUTSIDE.  H: [T][adapter_pitch(rank)] fp32;
+// H_out (nullable): [T][rank], rows of a request only.
+struct AdapterProjectArgs {
+    AdapterRows rows;
+    const void* X;
+    const void* F;
+    int64_t K;
+    bool bf16;
+    int32_t* row_adapter;
+    float* H;
+    float* H_out;
+};
+hipError_t launch_adapter_project(const AdapterProjectArgs& a, DeviceInfo& dev, hipStream_t stream);
+
+// base[s][m][n] = sum over the s-th part of k of A[m][k] B(n, k); A bf16 [M][K] row-major; B(n, k) = W[n][k] or, transposed,
+// W[k][n], with W [rows][cols] bf16 row-major or a bf16 operand in blocks of 256 x 64 (pitch: its zero-padded columns).
+struct AdapterBase {
+    const uint16_t* A;
+    const uint16_t* W;
+    bool transposed, blocked;
+    int64_t M, N, K;
+    float* planes;             // [split][M][N]
+    int split;
+};
+hipError_t launch_adapter_base_bf16(const AdapterBase& a, DeviceInfo& dev, hipStream_t stream);
+int adapter_base_split(int64_t M, int64_t N, int64_t K);
+
+// out[t][n] = sum_s planes[s][t][n] + sum_r H[t][r] F_a[r][n] for the rows of requests; out and F [count][rank][N] fp32 or bf16.
+struct AdapterJoinArgs {
+    const float* planes;
+    int split;
+    const int32_t* row_adapter;
+    const float* H;            // [T][adapter_pitch(rank)]
+    const void* F;
+    const int32_t* ranks;
+    int rank;
+    void* out;
+    bool bf16;
+    int64_t T, N;
+};
+hipError_t launch_adapter_join(const AdapterJoinArgs& a, hipStream_t stream);
+
+// out[a][r][c] = sum over the rows t of block a of H[t][r] G[t][c] for two such sums at once (r >= ranks[a]: zeros).
+struct AdapterOuter {
+    const float* H;
+    int64_t ldh;
+    const void* G;             // [T][C]
+    int64_t C;
+    float* out;                // [count][rank][C]
+};
+struct AdapterOuterArgs {
+    AdapterOuter sum[2];
+    const int32_t* row_adapter;
+    const int32_t* ranks;
+    int64_t count;
+    int rank;
+    bool bf16;
+    int64_t T;
+};
+hipError_t launch_adapter_outer(const AdapterOuterArgs& a, hipStream_t stream);
+
+// Norm over the tensors of a list and their scaling.  partial: grad_norm_partials(...) + 1 doubles.
+int64_t grad_norm_partials(const sfb_tensor* list, int64_t count);
+hipError_t launch_grad_norm(const sfb_tensor* list, int64_t count, double* partial, float* norm, hipStream_t stream);
+// (after launch_grad_norm on the same list and `partial`)
+hipError_t launch_clip(const sfb_tensor* list, int64_t count, const double* partial, double max_norm, hipStream_t stream);
+
+}  // namespace sfb

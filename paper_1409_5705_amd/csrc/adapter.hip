@@ -1,0 +1,449 @@
+// Factor blocks beside a shared projection (low-rank adapters of many requests): the contractions with the blocks.
+//
+//   project:  H[t][r] = scale_a sum_k X[t][k] F_a[r][k]            (a: the block of row t's request)
+//   join:     out[t][n] = base[t][n] + sum_r H[t][r] F'_a[r][n]    (base: the product with the shared matrix)
+//   outer:    out[a][r][c] = sum_{t of a} H[t][r] G[t][c]          (a block's gradients)
+//
+// Rows of one matrix belong to different blocks, so what one row holds (an infinity, a NaN) never meets another row's sum:
+// a product takes rows of ONE block at a time, and the others' results are dropped, not multiplied by zero.
+#include "adapter.h"
+#include "device.h"
+
+#include <algorithm>
+
+namespace sfb {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float bf16_float(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+
+// The request of row t, or -1 (empty requests are passed over: the last q with start[q] <= t).
+__device__ __forceinline__ int64_t request_of(const int64_t* start, int64_t requests, int64_t t)
+{
+    if (requests <= 0 || t < start[0] || t >= start[requests]) return -1;
+    int64_t lo = 0, hi = requests;
+    while (hi - lo > 1) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (start[mid] <= t)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    return lo;
+}
+__device__ __forceinline__ int rank_of(const int32_t* ranks, int rank, int64_t a)
+{
+    const int r = ranks ? ranks[a] : rank;
+    return r < 0 ? 0 : r < rank ? r : rank;
+}
+
+// 16 bytes of a row (eight bf16, four fp32) from element k on; what lies at or behind `end` is zero.  VEC: rows are 16-byte
+// aligned and `end` is a multiple of the elements.
+template <typename T, bool VEC>
+__device__ __forceinline__ u32x4 load_chunk(const T* row, int64_t k, int64_t end)
+{
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (VEC) {
+        if (k < end) v = *reinterpret_cast<const u32x4*>(row + k);
+    } else {
+        static_assert(VEC || sizeof(T) == 4, "bf16 rows are 16-byte aligned");
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (k + e < end) v[e] = *reinterpret_cast<const uint32_t*>(row + k + e);
+    }
+    return v;
+}
+
+// acc += sum of a 16-byte chunk of each of 16 rows a and 16 rows b: register i of lane (q, c) is row 4 q + i of a, row c of b.
+template <typename T>
+__device__ __forceinline__ floatx4 mfma_chunk(u32x4 a, u32x4 b, floatx4 acc)
+{
+    if constexpr (sizeof(T) == 2) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float((uint32_t)a[e]), __uint_as_float((uint32_t)b[e]), acc, 0, 0, 0);
+        return acc;
+    }
+}
+
+struct ProjectParams {
+    AdapterRows rows;
+    const void* X;
+    const void* F;
+    int64_t K;
+    int32_t* row_adapter;
+    float* H;
+    float* H_out;
+    int pitch;
+};
+
+constexpr int64_t MAX_BLOCKS = 1 << 22;      // workgroups of a launch (threads of a grid are counted in 32 bits)
+constexpr int PW = 8;      // wavefronts that share k
+
+// Rows ROWS * blockIdx.x .. of X against the 16 RT factors 16 RT * blockIdx.y ..; the eight wavefronts share k.
+template <typename T, bool VEC, int RT, int ROWS>
+__global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams p)
+{
+    constexpr int MT = (ROWS + 15) / 16, CE = 16 / (int)sizeof(T), STEP = 4 * CE;
+    __shared__ int row_of[32];
+    __shared__ floatx4 part[PW][MT * RT][64];
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t t0 = (int64_t)blockIdx.x * ROWS;
+    const int r0 = (int)blockIdx.y * 16 * RT;
+    const AdapterRows& rows = p.rows;
+    const int n_rows = (int)(rows.T - t0 < ROWS ? rows.T - t0 : ROWS);
+
+    if (tid < 32) {
+        int a = ROW_OUTSIDE;
+        if (tid < n_rows) {
+            const int64_t q = request_of(rows.start, rows.requests, t0 + tid);
+            if (q >= 0) {
+                a = rows.adapter[q];
+                if (a < 0 || a >= rows.count || rank_of(rows.ranks, rows.rank, a) == 0) a = ROW_NONE;
+            }
+            if (blockIdx.y == 0) p.row_adapter[t0 + tid] = a;
+        }
+        row_of[tid] = a;
+    }
+    __syncthreads();
+    const int mine = row_of[lane & 31];
+    // rows without a block: zeros
+    for (int i = tid; i < n_rows * 16 * RT; i += 64 * PW) {
+        const int t = i / (16 * RT), r = r0 + i % (16 * RT);
+        if (row_of[t] < 0 && r < p.pitch) {
+            p.H[(t0 + t) * p.pitch + r] = 0.f;
+            if (p.H_out && row_of[t] == ROW_NONE && r < rows.rank) p.H_out[(t0 + t) * rows.rank + r] = 0.f;
+        }
+    }
+
+    const int64_t steps = (p.K + STEP - 1) / STEP, per = (steps + PW - 1) / PW;
+    const int64_t k_begin = wave * per * STEP, k_end = k_begin + per * STEP < p.K ? k_begin + per * STEP : p.K;
+    const T* xr[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int t = 16 * m + l16;
+        xr[m] = static_cast<const T*>(p.X) + (t0 + (t < n_rows ? t : n_rows - 1)) * p.K;
+    }
+    uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(lane < 32 && mine >= 0);
+    while (left) {
+        const int a = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
+        const uint32_t now = (uint32_t)__builtin_amdgcn_ballot_w64(lane < 32 && mine == a);
+        left &= ~now;
+        const int rank = rank_of(rows.ranks, rows.rank, a);
+        const T* fr[RT];
+#pragma unroll
+        for (int f = 0; f < RT; ++f) {
+            const int r = r0 + 16 * f + l16;
+            fr[f] = static_cast<const T*>(p.F) + ((int64_t)a * rows.rank + (r < rank ? r : rank - 1)) * p.K;
+        }
+        floatx4 acc[MT][RT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int f = 0; f < RT; ++f) acc[m][f] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int64_t k = k_begin; k < k_end; k += STEP) {
+            u32x4 x[MT], w[RT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) x[m] = load_chunk<T, VEC>(xr[m], k + CE * quad, k_end);
+#pragma unroll
+            for (int f = 0; f < RT; ++f) w[f] = load_chunk<T, VEC>(fr[f], k + CE * quad, k_end);
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int f = 0; f < RT; ++f) acc[m][f] = mfma_chunk<T>(w[f], x[m], acc[m][f]);
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int f = 0; f < RT; ++f) part[wave][m * RT + f][lane] = acc[m][f];
+        __syncthreads();
+        const float s = rows.scale ? rows.scale[a] : 1.f;
+        for (int f = wave; f < MT * RT; f += PW) {
+            floatx4 sum = part[0][f][lane];
+#pragma unroll
+            for (int w = 1; w < PW; ++w) sum += part[w][f][lane];
+            const int t = 16 * (f / RT) + l16, r = r0 + 16 * (f % RT) + 4 * quad;
+            if (t < 32 && (now >> t & 1)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float h = r + i < rank ? s * sum[i] : 0.f;
+                    if (r + i < p.pitch) p.H[(t0 + t) * p.pitch + r + i] = h;
+                    if (p.H_out && r + i < rows.rank) p.H_out[(t0 + t) * rows.rank + r + i] = h;
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// A thread: 16 bytes of one row of the output.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void adapter_join_kernel(AdapterJoinArgs p, int blocks_n, int64_t t0)
+{
+    constexpr int CE = 16 / (int)sizeof(T);
+    const int64_t t = t0 + blockIdx.x / blocks_n, n = ((int64_t)(blockIdx.x % blocks_n) * 256 + threadIdx.x) * CE;
+    const int a = p.row_adapter[t];
+    if (a == ROW_OUTSIDE || n >= p.N) return;
+    const int live = (int)(p.N - n < CE ? p.N - n : CE);
+    float v[CE];
+#pragma unroll
+    for (int e = 0; e < CE; ++e) v[e] = 0.f;
+    for (int s = 0; s < p.split; ++s) {
+        const float* src = p.planes + ((int64_t)s * p.T + t) * p.N + n;
+        if (VEC) {
+#pragma unroll
+            for (int e = 0; e < CE; e += 4) {
+                const floatx4 x = *reinterpret_cast<const floatx4*>(src + e);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[e + i] += x[i];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < CE; ++e)
+                if (e < live) v[e] += src[e];
+        }
+    }
+    if (a >= 0) {
+        const int rank = rank_of(p.ranks, p.rank, a);
+        const T* F = static_cast<const T*>(p.F) + (int64_t)a * p.rank * p.N + n;
+        const float* h = p.H + t * adapter_pitch(p.rank);
+        float low[CE];
+#pragma unroll
+        for (int e = 0; e < CE; ++e) low[e] = 0.f;
+#pragma unroll 4
+        for (int r = 0; r < rank; ++r) {
+            const float hr = h[r];
+            const u32x4 f = load_chunk<T, VEC>(F + r * p.N, 0, live);
+#pragma unroll
+            for (int e = 0; e < CE; ++e) {
+                const uint32_t w = f[sizeof(T) == 2 ? e >> 1 : e];
+                low[e] = fmaf(hr, __uint_as_float(sizeof(T) == 4 ? w : (e & 1) ? w & 0xffff0000u : w << 16), low[e]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < CE; ++e) v[e] += low[e];
+    }
+    T* out = static_cast<T*>(p.out) + t * p.N + n;
+    if constexpr (sizeof(T) == 2) {
+        u32x4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+        *reinterpret_cast<u32x4*>(out) = o;
+    } else if (VEC) {
+        *reinterpret_cast<floatx4*>(out) = floatx4{v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+        for (int e = 0; e < CE; ++e)
+            if (e < live) out[e] = v[e];
+    }
+}
+
+constexpr int OW = 8, WINDOW = 4096;      // wavefronts; rows of which one list is made
+
+struct OuterParams {
+    AdapterOuter sum[2];
+    const int32_t* row_adapter;
+    const int32_t* ranks;
+    int64_t count;
+    int rank;
+    int64_t T;
+    unsigned tiles0, tiles;
+};
+
+// A tile of 16 CE columns and 16 RT factors of one block's gradient.  The workgroup lists the block's rows (WINDOW rows of the
+// matrix at a time), its wavefronts take four of them at a time: the fp32 MFMA's k.  Both operands come from memory in the
+// lanes' own order: lane (q, c) loads 16 bytes of row q, columns CE c .. , which are the columns CE c + f of MFMA f.
+template <typename T, bool VEC, int RT>
+__global__ __launch_bounds__(64 * OW) void adapter_outer_kernel(OuterParams p)
+{
+    constexpr int CE = 16 / (int)sizeof(T), U = 2;
+    __shared__ int32_t list[WINDOW];
+    __shared__ int counts[OW];
+    __shared__ floatx4 part[OW][CE][64];
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const unsigned tile = blockIdx.x % p.tiles;
+    const int64_t block = blockIdx.x / p.tiles;
+    const int a = (int)(block % p.count), r0 = (int)(block / p.count) * 16 * RT;
+    const AdapterOuter& sum = p.sum[tile >= p.tiles0 ? 1 : 0];
+    const int64_t c0 = (int64_t)(tile >= p.tiles0 ? tile - p.tiles0 : tile) * (16 * CE) + CE * l16;
+    const int rank = rank_of(p.ranks, p.rank, a);
+
+    floatx4 acc[RT][CE];
+#pragma unroll
+    for (int f = 0; f < RT; ++f)
+#pragma unroll
+        for (int e = 0; e < CE; ++e) acc[f][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int64_t w0 = 0; w0 < p.T && r0 < rank; w0 += WINDOW) {
+        // the rows of the window that belong to the block, in their order
+        constexpr int PER = WINDOW / (64 * OW);
+        int found = 0;
+        uint32_t bits = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int64_t t = w0 + tid * PER + i;
+            if (t < p.T && p.row_adapter[t] == a) {
+                bits |= 1u << i;
+                ++found;
+            }
+        }
+        int before = found;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(before, d);
+            if (lane >= d) before += o;
+        }
+        if (lane == 63) counts[wave] = before;
+        before -= found;
+        __syncthreads();
+        int total = 0;
+#pragma unroll
+        for (int w = 0; w < OW; ++w) {
+            const int c = counts[w];
+            if (w < wave) before += c;
+            total += c;
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (bits >> i & 1) list[before++] = tid * PER + i;
+        __syncthreads();
+        for (int i0 = wave * 4 * U; i0 < total; i0 += OW * 4 * U) {
+            u32x4 g[U];
+            float h[U][RT];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + 4 * u + quad;
+                const bool in = i < total;
+                const int64_t t = w0 + list[in ? i : 0];
+                g[u] = u32x4{0u, 0u, 0u, 0u};
+                if (in) g[u] = load_chunk<T, VEC>(static_cast<const T*>(sum.G) + t * sum.C, c0, sum.C);
+#pragma unroll
+                for (int f = 0; f < RT; ++f) {
+                    const int r = r0 + 16 * f + l16;
+                    h[u][f] = in && r < rank ? sum.H[t * sum.ldh + r] : 0.f;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < CE; ++e) {
+                    const uint32_t w = g[u][sizeof(T) == 2 ? e >> 1 : e];
+                    const float ge = __uint_as_float(sizeof(T) == 4 ? w : (e & 1) ? w & 0xffff0000u : w << 16);
+#pragma unroll
+                    for (int f = 0; f < RT; ++f) acc[f][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(h[u][f], ge, acc[f][e], 0, 0, 0);
+                }
+        }
+        __syncthreads();
+    }
+    // register i of lane (q, c): factor 4 q + i, column CE c + e of acc[.][e]
+#pragma unroll
+    for (int f = 0; f < RT; ++f) {
+#pragma unroll
+        for (int e = 0; e < CE; ++e) part[wave][e][lane] = acc[f][e];
+        __syncthreads();
+        for (int e = wave; e < CE; e += OW) {
+            floatx4 s = part[0][e][lane];
+#pragma unroll
+            for (int w = 1; w < OW; ++w) s += part[w][e][lane];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = r0 + 16 * f + 4 * quad + i;
+                if (r < p.rank && c0 + e < sum.C) sum.out[((int64_t)a * p.rank + r) * sum.C + c0 + e] = r < rank ? s[i] : 0.f;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+template <typename T, bool VEC, int RT>
+hipError_t project_rows(const ProjectParams& p, int rows, hipStream_t stream)
+{
+    const unsigned y = (unsigned)std::max(1, (p.pitch + 16 * RT - 1) / (16 * RT));
+    const int64_t x = (p.rows.T + rows - 1) / rows;
+    if (x > MAX_BLOCKS) return hipErrorInvalidConfiguration;
+    if (rows == 1)
+        adapter_project_kernel<T, VEC, RT, 1><<<dim3((unsigned)x, y), 64 * PW, 0, stream>>>(p);
+    else
+        adapter_project_kernel<T, VEC, RT, 32><<<dim3((unsigned)x, y), 64 * PW, 0, stream>>>(p);
+    return hipGetLastError();
+}
+template <typename T, bool VEC>
+hipError_t project_rank(const ProjectParams& p, int rows, hipStream_t stream)
+{
+    if (p.pitch <= 16) return project_rows<T, VEC, 1>(p, rows, stream);
+    if (p.pitch <= 32) return project_rows<T, VEC, 2>(p, rows, stream);
+    return project_rows<T, VEC, 4>(p, rows, stream);
+}
+
+template <typename T, bool VEC>
+hipError_t outer_rank(const OuterParams& p, hipStream_t stream)
+{
+    const int rt = p.rank <= 16 ? 1 : p.rank <= 32 ? 2 : 4;
+    const int64_t blocks = (int64_t)p.tiles * p.count * ((p.rank + 16 * rt - 1) / (16 * rt));
+    if (blocks > MAX_BLOCKS) return hipErrorInvalidConfiguration;
+    if (rt == 1)
+        adapter_outer_kernel<T, VEC, 1><<<(unsigned)blocks, 64 * OW, 0, stream>>>(p);
+    else if (rt == 2)
+        adapter_outer_kernel<T, VEC, 2><<<(unsigned)blocks, 64 * OW, 0, stream>>>(p);
+    else
+        adapter_outer_kernel<T, VEC, 4><<<(unsigned)blocks, 64 * OW, 0, stream>>>(p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_adapter_project(const AdapterProjectArgs& a, DeviceInfo&, hipStream_t stream)
+{
+    if (a.rows.T <= 0) return hipSuccess;
+    ProjectParams p = {a.rows, a.X, a.F, a.K, a.row_adapter, a.H, a.H_out, adapter_pitch(a.rows.rank)};
+    // A tile of rows is gone through once for every block in it: rows of requests of a few tokens go one by one.
+    const int rows = a.rows.requests * 8 > a.rows.T ? 1 : 32;
+    if (a.bf16) return project_rank<uint16_t, true>(p, rows, stream);
+    return a.K % 4 == 0 ? project_rank<float, true>(p, rows, stream) : project_rank<float, false>(p, rows, stream);
+}
+
+hipError_t launch_adapter_join(const AdapterJoinArgs& a, hipStream_t stream)
+{
+    if (a.T <= 0) return hipSuccess;
+    const int ce = a.bf16 ? 8 : 4;
+    const int blocks_n = (int)((a.N + 256 * ce - 1) / (256 * ce));
+    const int64_t rows = std::max<int64_t>(1, MAX_BLOCKS / blocks_n);
+    for (int64_t t0 = 0; t0 < a.T; t0 += rows) {
+        const unsigned blocks = (unsigned)(std::min(rows, a.T - t0) * blocks_n);
+        if (a.bf16)
+            adapter_join_kernel<uint16_t, true><<<blocks, 256, 0, stream>>>(a, blocks_n, t0);
+        else if (a.N % 4 == 0)
+            adapter_join_kernel<float, true><<<blocks, 256, 0, stream>>>(a, blocks_n, t0);
+        else
+            adapter_join_kernel<float, false><<<blocks, 256, 0, stream>>>(a, blocks_n, t0);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_adapter_outer(const AdapterOuterArgs& a, hipStream_t stream)
+{
+    if (a.count <= 0) return hipSuccess;
+    const int64_t width = 16 * (a.bf16 ? 8 : 4);
+    OuterParams p = {};
+    p.sum[0] = a.sum[0];
+    p.sum[1] = a.sum[1];
+    p.row_adapter = a.row_adapter;
+    p.ranks = a.ranks;
+    p.count = a.count;
+    p.rank = a.rank;
+    p.T = a.T;
+    p.tiles0 = (unsigned)((a.sum[0].C + width - 1) / width);
+    p.tiles = p.tiles0 + (unsigned)((a.sum[1].C + width - 1) / width);
+    if (a.bf16) return outer_rank<uint16_t, true>(p, stream);
+    return a.sum[0].C % 4 == 0 && a.sum[1].C % 4 == 0 ? outer_rank<float, true>(p, stream) : outer_rank<float, false>(p, stream);
+}
+
+}  // namespace sfb

@@ -579,6 +579,7 @@ hipError_t launch_gemm_f32x3(const GemmF32Args& a, GemmF32Params p, const GemmF3
     if (!aks && !bks && a.epilogue == EPI_SHRINK) return launch_any<false, false, EPI_SHRINK>(p, *a.dev, 1, plan, stream);
     if (!aks && bks && a.epilogue == EPI_RESID) return launch_any<false, true, EPI_RESID>(p, *a.dev, 2, plan, stream);
     if (aks && bks && a.epilogue == EPI_RMW) return launch_any<true, true, EPI_RMW>(p, *a.dev, 3, plan, stream);
+    if (!aks && bks && a.epilogue == EPI_STORE) return launch_any<false, true, EPI_STORE>(p, *a.dev, 4, plan, stream);
     return hipErrorInvalidValue;
 }
 

@@ -7,6 +7,7 @@
 
 #include <new>
 
+#include "adapter.h"
 #include "kernels.h"
 
 // Kernel groups reported by the optional per-kernel timing.
@@ -32,12 +33,19 @@ enum KernelId : int {
     KID_SDCA,
     KID_DUAL_TO_PRIMAL,
     KID_APPLY_GATHER,
+    KID_ADAPTER_PROJECT,
+    KID_ADAPTER_BASE,
+    KID_ADAPTER_JOIN,
+    KID_ADAPTER_OUTER,
+    KID_GRAD_NORM,
+    KID_CLIP,
     KID_COUNT
 };
 static const char* const kKernelNames[KID_COUNT] = {
     "mlr_forward_bf16", "apply_bf16", "apply_bf16_transpose", "mlr_softmax", "gemm_f32_store", "gemm_f32_rmw(apply)", "gemm_f32_resid",
     "gemm_f32_shrink", "diff", "dml_scale", "fill", "prox_rows", "power_iteration", "copy", "shadow_convert", "scale_rows",
-    "csr_to_operand", "csr_forward_gather", "sdca_mlr", "dual_to_primal", "apply_gather"};
+    "csr_to_operand", "csr_forward_gather", "sdca_mlr", "dual_to_primal", "apply_gather",
+    "adapter_project", "adapter_base", "adapter_join", "adapter_outer", "grad_norm", "clip"};
 
 struct ProfSpan {
     hipEvent_t t0, t1;
@@ -987,6 +995,280 @@ int sfb_prox_rows(sfb_ctx* ctx, float* W, int64_t J, int64_t D, int32_t mode)
     if (ctx->shadow_buf && ctx->shadow_W == W && ctx->shadow_J == J && ctx->shadow_D == D)
         SFB_RUN(KID_SHADOW, sfb::launch_shadow_from_w(W, ctx->shadow_buf, J, D, ctx->stream));
     return SFB_OK;
+}
+
+// ---- factor blocks beside a shared matrix ------------------------------------------------------------------------------
+
+// Makes the context's device current for a call and the caller's again after it.
+struct DeviceScope {
+    int prev = -1;
+    hipError_t status;
+    explicit DeviceScope(int device)
+    {
+        status = hipGetDevice(&prev);
+        if (status == hipSuccess && prev != device)
+            status = hipSetDevice(device);
+        else
+            prev = -1;
+    }
+    ~DeviceScope()
+    {
+        if (prev >= 0) (void)hipSetDevice(prev);
+    }
+};
+
+static int check_adapters(int64_t J, int64_t D, int64_t T, const sfb_adapters* ad)
+{
+    constexpr int64_t BF16_COLS = 4194304;      // a tile's rows are addressed with 32-bit offsets
+    if (!ad || J <= 0 || D <= 0 || T < 0 || !valid_dtype(ad->dtype)) return SFB_EINVAL;
+    if (T > INT32_MAX || J > INT32_MAX || D > INT32_MAX) return SFB_EINVAL;
+    if (ad->dtype == SFB_BF16 && (J % 8 != 0 || D % 8 != 0 || J > BF16_COLS || D > BF16_COLS)) return SFB_EINVAL;
+    if (ad->count < 0 || ad->count > 65536) return SFB_EINVAL;
+    if (ad->rank < (ad->count > 0 ? 1 : 0) || ad->rank > SFB_ADAPTER_MAX_RANK) return SFB_EINVAL;
+    return SFB_OK;
+}
+
+// The workspace of either call: the block of each row, the projections (forward H; backward H and dH), the product with the
+// shared matrix (N columns, contracted over K) and what its contraction needs itself.
+struct AdapterLayout {
+    int64_t off_h, off_dh, off_planes, off_partial, total;
+    int split;
+};
+static AdapterLayout adapter_layout(int64_t T, int64_t N, int64_t K, const sfb_adapters* ad, bool backward)
+{
+    AdapterLayout l;
+    const int64_t h = round_up(T * sfb::adapter_pitch(ad->rank) * 4);
+    l.off_h = round_up(T * 4);
+    l.off_dh = l.off_h + h;
+    l.off_planes = l.off_dh + (backward ? h : 0);
+    l.split = ad->dtype == SFB_BF16 ? sfb::adapter_base_split(T, N, K) : 1;
+    l.off_partial = l.off_planes + round_up(l.split * T * N * 4);
+    l.total = l.off_partial + (ad->dtype == SFB_F32 && T > 0 ? round_up(sfb::gemm_f32_partial_bytes(T, N, K)) : 0);
+    return l;
+}
+
+int64_t sfb_adapter_forward_workspace_bytes(int64_t J, int64_t D, int64_t T, const sfb_adapters* ad)
+{
+    const int rc = check_adapters(J, D, T, ad);
+    return rc != SFB_OK ? rc : adapter_layout(T, J, D, ad, false).total;
+}
+int64_t sfb_adapter_backward_workspace_bytes(int64_t J, int64_t D, int64_t T, const sfb_adapters* ad)
+{
+    const int rc = check_adapters(J, D, T, ad);
+    return rc != SFB_OK ? rc : adapter_layout(T, D, J, ad, true).total;
+}
+
+// Arguments that both calls have.  *Wb: the bf16 matrix that bf16 blocks go with, *blocked: it is in the operand layout.
+static int check_adapter_call(const sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J, int64_t D, int64_t T, const sfb_adapters* ad,
+                              const sfb_requests* rq, const uint16_t** Wb, bool* blocked)
+{
+    if (!ctx) return SFB_EINVAL;
+    const int rc = check_adapters(J, D, T, ad);
+    if (rc != SFB_OK) return rc;
+    if (ad->count > 0 && (!ad->U || !ad->V || !aligned16(ad->U) || !aligned16(ad->V) || !aligned16(ad->ranks) || !aligned16(ad->scale)))
+        return SFB_EINVAL;
+    if (!rq || rq->count < 0 || !aligned16(rq->start) || !aligned16(rq->adapter)) return SFB_EINVAL;
+    if (rq->count > 0 && (!rq->start || !rq->adapter)) return SFB_EINVAL;
+    if (!W || !aligned16(W) || !valid_dtype(w_dtype)) return SFB_EINVAL;
+    *Wb = nullptr;
+    *blocked = false;
+    const float* Wf = static_cast<const float*>(W);
+    if (ad->dtype == SFB_F32) return w_dtype == SFB_F32 && !is_split(ctx, Wf) ? SFB_OK : SFB_EINVAL;
+    if (w_dtype == SFB_BF16) {
+        *Wb = static_cast<const uint16_t*>(W);
+        return SFB_OK;
+    }
+    if (!ctx->shadow_buf || ctx->shadow_W != Wf || ctx->shadow_J != J || ctx->shadow_D != D) return SFB_EINVAL;
+    *Wb = ctx->shadow_buf;
+    *blocked = true;
+    return SFB_OK;
+}
+
+// out = src times the shared matrix (transposed: by its columns) + H times the blocks' `factors`.
+static int adapter_output(sfb_ctx* ctx, const AdapterLayout& l, const void* src, const void* W, const uint16_t* Wb, bool blocked,
+                          bool transposed, int64_t T, int64_t N, int64_t K, const sfb_adapters* ad, const void* factors, const float* H,
+                          void* out)
+{
+    const bool bf16 = ad->dtype == SFB_BF16;
+    float* planes = reinterpret_cast<float*>(ctx->ws + l.off_planes);
+    sfb::AdapterJoinArgs j = {};
+    j.planes = planes;
+    j.split = l.split;
+    if (bf16) {
+        sfb::AdapterBase b = {};
+        b.A = static_cast<const uint16_t*>(src);
+        b.W = Wb;
+        b.transposed = transposed;
+        b.blocked = blocked;
+        b.M = T; b.N = N; b.K = K;
+        b.planes = planes;
+        b.split = l.split;
+        SFB_RUN(KID_ADAPTER_BASE, sfb::launch_adapter_base_bf16(b, ctx->dev, ctx->stream));
+    } else {
+        int parts = 1;
+        sfb::GemmF32Args g = {};
+        g.dev = &ctx->dev;
+        g.A = static_cast<const float*>(src); g.lda = K; g.a_kstrided = false;
+        g.B = static_cast<const float*>(W); g.ldb = transposed ? N : K; g.b_kstrided = transposed;
+        g.C = planes; g.ldc = N;
+        g.M = T; g.N = N; g.K = K;
+        g.epilogue = sfb::EPI_STORE;
+        if (l.total > l.off_partial) g.partial = reinterpret_cast<float*>(ctx->ws + l.off_partial);
+        g.parts = &parts;
+        SFB_RUN(KID_ADAPTER_BASE, sfb::launch_gemm_f32(g, ctx->stream));
+        if (parts > 1) {      // the join adds them up
+            j.planes = g.partial;
+            j.split = parts;
+        }
+    }
+    j.row_adapter = reinterpret_cast<const int32_t*>(ctx->ws);
+    j.H = H;
+    j.F = factors;
+    j.ranks = ad->ranks;
+    j.rank = ad->rank;
+    j.out = out;
+    j.bf16 = bf16;
+    j.T = T;
+    j.N = N;
+    SFB_RUN(KID_ADAPTER_JOIN, sfb::launch_adapter_join(j, ctx->stream));
+    return SFB_OK;
+}
+
+static sfb::AdapterProjectArgs project_args(sfb_ctx* ctx, int64_t T, const sfb_adapters* ad, const sfb_requests* rq)
+{
+    sfb::AdapterProjectArgs a = {};
+    a.rows.start = rq->start;
+    a.rows.adapter = rq->adapter;
+    a.rows.requests = rq->count;
+    a.rows.ranks = ad->ranks;
+    a.rows.scale = ad->scale;
+    a.rows.count = ad->count;
+    a.rows.rank = ad->rank;
+    a.rows.T = T;
+    a.bf16 = ad->dtype == SFB_BF16;
+    a.row_adapter = reinterpret_cast<int32_t*>(ctx->ws);
+    return a;
+}
+
+int sfb_adapter_forward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J, int64_t D, const void* X, int64_t T,
+                        const sfb_adapters* ad, const sfb_requests* rq, void* Y, float* H)
+{
+    const uint16_t* Wb;
+    bool blocked;
+    const int rc = check_adapter_call(ctx, W, w_dtype, J, D, T, ad, rq, &Wb, &blocked);
+    if (rc != SFB_OK) return rc;
+    if (!aligned16(H)) return SFB_EINVAL;
+    if (T == 0 || rq->count == 0) return SFB_OK;
+    if (!X || !Y || !aligned16(X) || !aligned16(Y)) return SFB_EINVAL;
+    const AdapterLayout l = adapter_layout(T, J, D, ad, false);
+    if (!ctx->ws || ctx->ws_bytes < l.total) return SFB_ENOWS;
+    const DeviceScope scope(ctx->device);
+    SFB_TRY(scope.status);
+    sfb::AdapterProjectArgs a = project_args(ctx, T, ad, rq);
+    a.X = X;
+    a.F = ad->V;
+    a.K = D;
+    a.H = reinterpret_cast<float*>(ctx->ws + l.off_h);
+    a.H_out = H;
+    SFB_RUN(KID_ADAPTER_PROJECT, sfb::launch_adapter_project(a, ctx->dev, ctx->stream));
+    return adapter_output(ctx, l, X, W, Wb, blocked, false, T, J, D, ad, ad->U, a.H, Y);
+}
+
+int sfb_adapter_backward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J, int64_t D, const void* X, const void* dY, int64_t T,
+                         const sfb_adapters* ad, const sfb_requests* rq, const float* H, void* dX, float* dU, float* dV)
+{
+    const uint16_t* Wb;
+    bool blocked;
+    int rc = check_adapter_call(ctx, W, w_dtype, J, D, T, ad, rq, &Wb, &blocked);
+    if (rc != SFB_OK) return rc;
+    if (!aligned16(H) || !aligned16(dX) || !aligned16(dU) || !aligned16(dV) || (dU == nullptr) != (dV == nullptr)) return SFB_EINVAL;
+    const bool grads = dU && ad->count > 0;
+    if (!dX && !grads) return SFB_OK;
+    const bool rows = T > 0 && rq->count > 0;
+    if (rows && (!X || !dY || !aligned16(X) || !aligned16(dY))) return SFB_EINVAL;
+    if (!rows) T = 0;
+    const AdapterLayout l = adapter_layout(T, D, J, ad, true);
+    if (rows && (!ctx->ws || ctx->ws_bytes < l.total)) return SFB_ENOWS;
+    const DeviceScope scope(ctx->device);
+    SFB_TRY(scope.status);
+    sfb::AdapterProjectArgs a = project_args(ctx, T, ad, rq);
+    float* Hw = reinterpret_cast<float*>(ctx->ws + l.off_h);
+    float* dH = reinterpret_cast<float*>(ctx->ws + l.off_dh);
+    if (grads && !H) {
+        a.X = X;
+        a.F = ad->V;
+        a.K = D;
+        a.H = Hw;
+        SFB_RUN(KID_ADAPTER_PROJECT, sfb::launch_adapter_project(a, ctx->dev, ctx->stream));
+    }
+    a.X = dY;
+    a.F = ad->U;
+    a.K = J;
+    a.H = dH;
+    SFB_RUN(KID_ADAPTER_PROJECT, sfb::launch_adapter_project(a, ctx->dev, ctx->stream));
+    if (dX && rows) {
+        rc = adapter_output(ctx, l, dY, W, Wb, blocked, true, T, D, J, ad, ad->V, dH, dX);
+        if (rc != SFB_OK) return rc;
+    }
+    if (!grads) return SFB_OK;
+    sfb::AdapterOuterArgs o = {};
+    o.sum[0] = {H ? H : Hw, H ? ad->rank : sfb::adapter_pitch(ad->rank), dY, J, dU};
+    o.sum[1] = {dH, sfb::adapter_pitch(ad->rank), X, D, dV};
+    o.row_adapter = reinterpret_cast<const int32_t*>(ctx->ws);
+    o.ranks = ad->ranks;
+    o.count = ad->count;
+    o.rank = ad->rank;
+    o.bf16 = a.bf16;
+    o.T = T;
+    SFB_RUN(KID_ADAPTER_OUTER, sfb::launch_adapter_outer(o, ctx->stream));
+    return SFB_OK;
+}
+
+// ---- norm and clipping of gradients ------------------------------------------------------------------------------------
+
+static int check_list(const sfb_tensor* list, int64_t count, bool clip)
+{
+    if (count < 0 || (count > 0 && !list)) return SFB_EINVAL;
+    for (int64_t i = 0; i < count; ++i) {
+        const sfb_tensor& t = list[i];
+        if (t.n < 0 || t.n > (int64_t(1) << 48) || !valid_dtype(t.dtype)) return SFB_EINVAL;
+        if (t.n == 0) continue;
+        const uintptr_t off = t.dtype == SFB_BF16 ? 1u : 3u;
+        if (!t.src || (reinterpret_cast<uintptr_t>(t.src) & off)) return SFB_EINVAL;
+        if (clip && (!t.dst || (reinterpret_cast<uintptr_t>(t.dst) & off))) return SFB_EINVAL;
+    }
+    return SFB_OK;
+}
+
+int64_t sfb_grad_norm_workspace_bytes(const sfb_tensor* list, int64_t count)
+{
+    const int rc = check_list(list, count, false);
+    return rc != SFB_OK ? rc : round_up((sfb::grad_norm_partials(list, count) + 1) * 8);
+}
+
+static int grad_norm_impl(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, bool clip, float max_norm, float* norm)
+{
+    if (!ctx || !norm || (reinterpret_cast<uintptr_t>(norm) & 3u)) return SFB_EINVAL;
+    const int rc = check_list(list, count, clip);
+    if (rc != SFB_OK) return rc;
+    if (!ctx->ws || ctx->ws_bytes < round_up((sfb::grad_norm_partials(list, count) + 1) * 8)) return SFB_ENOWS;
+    const DeviceScope scope(ctx->device);
+    SFB_TRY(scope.status);
+    double* partial = reinterpret_cast<double*>(ctx->ws);
+    SFB_RUN(KID_GRAD_NORM, sfb::launch_grad_norm(list, count, partial, norm, ctx->stream));
+    if (clip) SFB_RUN(KID_CLIP, sfb::launch_clip(list, count, partial, (double)max_norm, ctx->stream));
+    return SFB_OK;
+}
+
+int sfb_grad_norm(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, float* norm)
+{
+    return grad_norm_impl(ctx, list, count, false, 0.f, norm);
+}
+
+int sfb_clip_grads(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, float max_norm, float* norm)
+{
+    if (!(max_norm >= 0.f)) return SFB_EINVAL;
+    return grad_norm_impl(ctx, list, count, true, max_norm, norm);
 }
 
 const char* sfb_strerror(int code)

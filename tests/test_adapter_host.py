@@ -1,0 +1,114 @@
+"""The argument checks of the adapter and clipping calls, which all come before the first device call: a context of zeros (no
+workspace, nothing attached) refuses wrong arguments with SFB_EINVAL and right ones with SFB_ENOWS."""
+import ctypes
+
+import pytest
+
+P = 4096          # any 16-byte aligned address: nothing is read through it
+
+
+@pytest.fixture(scope="module")
+def sfb():
+    import os
+    import paper_1409_5705_amd as m
+    if not os.path.exists(m.binding.LIB_PATH):
+        from paper_1409_5705_amd.build import build_library
+        build_library()
+    m.lib()
+    return m
+
+
+@pytest.fixture()
+def ctx():
+    return ctypes.create_string_buffer(8192)
+
+
+def adapters(sfb, U=P, V=P, ranks=None, scale=None, count=3, rank=8, dtype=1):
+    a = sfb.binding.sfb_adapters()
+    a.U, a.V, a.ranks, a.scale, a.count, a.rank, a.dtype = U, V, ranks, scale, count, rank, dtype
+    return a
+
+
+def requests(sfb, start=P, adapter=P, count=2):
+    r = sfb.binding.sfb_requests()
+    r.start, r.adapter, r.count = start, adapter, count
+    return r
+
+
+def forward(sfb, ctx, ad=None, rq=None, W=P, w_dtype=1, J=64, D=72, X=P, T=10, Y=P, H=None):
+    ad = adapters(sfb) if ad is None else ad
+    rq = requests(sfb) if rq is None else rq
+    return sfb.lib().sfb_adapter_forward(ctx, W, w_dtype, J, D, X, T, ctypes.byref(ad), ctypes.byref(rq), Y, H)
+
+
+def backward(sfb, ctx, ad=None, rq=None, W=P, w_dtype=1, J=64, D=72, X=P, dY=P, T=10, H=None, dX=P, dU=P, dV=P):
+    ad = adapters(sfb) if ad is None else ad
+    rq = requests(sfb) if rq is None else rq
+    return sfb.lib().sfb_adapter_backward(ctx, W, w_dtype, J, D, X, dY, T, ctypes.byref(ad), ctypes.byref(rq), H, dX, dU, dV)
+
+
+@pytest.mark.parametrize("call", [forward, backward])
+def test_refusals_of_both(sfb, ctx, call):
+    assert call(sfb, None) == sfb.SFB_EINVAL
+    assert call(sfb, ctx) == sfb.SFB_ENOWS
+    for a in (dict(U=None), dict(V=None), dict(U=P + 8), dict(V=P + 2), dict(ranks=P + 4), dict(scale=P + 4), dict(count=-1),
+              dict(count=65537), dict(rank=0), dict(rank=257), dict(dtype=2), dict(dtype=-1)):
+        assert call(sfb, ctx, ad=adapters(sfb, **a)) == sfb.SFB_EINVAL, a
+    for r in (dict(start=None), dict(adapter=None), dict(start=P + 8), dict(adapter=P + 4), dict(count=-1)):
+        assert call(sfb, ctx, rq=requests(sfb, **r)) == sfb.SFB_EINVAL, r
+    for k in (dict(W=None), dict(W=P + 8), dict(w_dtype=0), dict(w_dtype=3), dict(J=0), dict(D=-8), dict(J=60), dict(D=60),
+              dict(J=4194312), dict(D=4194312), dict(T=-1), dict(X=None), dict(X=P + 2), dict(H=P + 4), dict(T=1 << 31)):
+        assert call(sfb, ctx, **k) == sfb.SFB_EINVAL, k
+    # fp32: any sizes, an fp32 matrix
+    assert call(sfb, ctx, ad=adapters(sfb, dtype=0), w_dtype=0, J=61, D=3) == sfb.SFB_ENOWS
+    assert call(sfb, ctx, ad=adapters(sfb, dtype=0), w_dtype=1) == sfb.SFB_EINVAL
+    # a pool without blocks is not looked at
+    assert call(sfb, ctx, ad=adapters(sfb, U=None, V=None, count=0, rank=0)) == sfb.SFB_ENOWS
+
+
+def test_refusals_of_one(sfb, ctx):
+    assert forward(sfb, ctx, Y=None) == sfb.SFB_EINVAL and forward(sfb, ctx, Y=P + 2) == sfb.SFB_EINVAL
+    assert forward(sfb, ctx, T=0, X=None, Y=None) == sfb.SFB_OK
+    assert forward(sfb, ctx, rq=requests(sfb, start=None, adapter=None, count=0), X=None, Y=None) == sfb.SFB_OK
+    for k in (dict(dY=None), dict(dY=P + 8), dict(dX=P + 8), dict(dU=P + 4), dict(dV=P + 4), dict(dU=None), dict(dV=None)):
+        assert backward(sfb, ctx, **k) == sfb.SFB_EINVAL, k
+    assert backward(sfb, ctx, dX=None, dU=None, dV=None) == sfb.SFB_OK          # nothing wanted
+    assert backward(sfb, ctx, dX=None) == sfb.SFB_ENOWS and backward(sfb, ctx, dU=None, dV=None) == sfb.SFB_ENOWS
+
+
+def test_workspace_queries(sfb):
+    L = sfb.lib()
+    for q in (L.sfb_adapter_forward_workspace_bytes, L.sfb_adapter_backward_workspace_bytes):
+        one = q(64, 72, 10, ctypes.byref(adapters(sfb)))
+        assert one > 0 and one % 256 == 0
+        assert q(64, 72, 1000, ctypes.byref(adapters(sfb))) > one
+        assert q(64, 72, 0, ctypes.byref(adapters(sfb))) >= 0
+        assert q(64, 72, 10, None) == sfb.SFB_EINVAL
+        assert q(64, 70, 10, ctypes.byref(adapters(sfb))) == sfb.SFB_EINVAL
+        assert q(64, 70, 10, ctypes.byref(adapters(sfb, dtype=0))) > 0
+        assert q(64, 72, -1, ctypes.byref(adapters(sfb))) == sfb.SFB_EINVAL
+
+
+def test_refusals_of_clipping(sfb, ctx):
+    L = sfb.lib()
+
+    def items(*rows):
+        t = (sfb.binding.sfb_tensor * max(1, len(rows)))()
+        for k, (src, dst, n, dtype) in enumerate(rows):
+            t[k].src, t[k].dst, t[k].n, t[k].dtype = src, dst, n, dtype
+        return t, len(rows)
+
+    good = [(P, P, 5, 0), (P + 2, P + 2, 9, 1), (None, None, 0, 1)]
+    assert L.sfb_grad_norm(ctx, *items(*good), P) == sfb.SFB_ENOWS
+    assert L.sfb_clip_grads(ctx, *items(*good), 1.0, P) == sfb.SFB_ENOWS
+    assert L.sfb_grad_norm(ctx, *items((P, None, 5, 0)), P) == sfb.SFB_ENOWS          # dst is not looked at
+    assert L.sfb_clip_grads(ctx, *items((P, None, 5, 0)), 1.0, P) == sfb.SFB_EINVAL
+    for bad in ((None, P, 5, 0), (P + 2, P, 5, 0), (P + 1, P, 5, 1), (P, P, -1, 0), (P, P, 5, 2)):
+        assert L.sfb_grad_norm(ctx, *items(bad), P) == sfb.SFB_EINVAL, bad
+        assert L.sfb_grad_norm_workspace_bytes(*items(bad)) == sfb.SFB_EINVAL
+    for bound in (-1.0, float("nan")):
+        assert L.sfb_clip_grads(ctx, *items(*good), bound, P) == sfb.SFB_EINVAL
+    assert L.sfb_grad_norm(None, *items(*good), P) == sfb.SFB_EINVAL
+    assert L.sfb_grad_norm(ctx, *items(*good), None) == sfb.SFB_EINVAL
+    assert L.sfb_grad_norm(ctx, None, 1, P) == sfb.SFB_EINVAL and L.sfb_grad_norm(ctx, None, -1, P) == sfb.SFB_EINVAL
+    assert L.sfb_grad_norm_workspace_bytes(None, 0) > 0

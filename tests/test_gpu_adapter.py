@@ -1,0 +1,319 @@
+"""Factor blocks beside a shared matrix (sfb_adapter_forward, sfb_adapter_backward) against the formulas in 64 bits: lengths from
+none to many tiles, odd sizes, ranks from 0 to 256, blocks shared by requests, rows of no request, and not-a-numbers in
+every place that the calls must not look at."""
+import numpy as np
+import pytest
+import torch
+
+import adapter_ref as A
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+SENTINEL = 12345.0
+
+
+@pytest.fixture(scope="module")
+def sfb():
+    import paper_1409_5705_amd as m
+    m.lib()
+    return m
+
+
+@pytest.fixture(scope="module")
+def ctx(sfb):
+    c = sfb.Context(0)
+    yield c
+    c.close()
+
+
+KEYS = ("W", "X", "dY", "U", "V", "start", "adapter", "ranks", "scale")
+
+
+def to_dev(c):
+    return {k: c[k].to("cuda:0") for k in KEYS}
+
+
+def outputs(c):
+    full = lambda *s, dt=F32: torch.full(s, SENTINEL, dtype=dt, device="cuda:0")  # noqa: E731
+    return dict(Y=full(c["T"], c["J"], dt=c["dtype"]), H=full(c["T"], c["R"]), dX=full(c["T"], c["D"], dt=c["dtype"]),
+                dU=full(c["n"], c["R"], c["J"]), dV=full(c["n"], c["R"], c["D"]))
+
+
+def forward(ctx, d, o, W=None, H=True):
+    ctx.sfb_adapter_forward(d["W"] if W is None else W, d["X"], d["start"], d["adapter"], d["U"], d["V"], o["Y"], ranks=d["ranks"],
+                            scale=d["scale"], H=o["H"] if H else None)
+
+
+def backward(ctx, d, o, W=None, H=None):
+    ctx.sfb_adapter_backward(d["W"] if W is None else W, d["X"], d["dY"], d["start"], d["adapter"], d["U"], d["V"], o["dX"], o["dU"],
+                             o["dV"], ranks=d["ranks"], scale=d["scale"], H=H)
+
+
+def compare(c, o, names=("Y", "H", "dX", "dU", "dV")):
+    ref, rows = A.reference(c)
+    outside = torch.ones(c["T"], dtype=torch.bool)
+    outside[rows] = False
+    for k in names:
+        per_row = k in ("Y", "H", "dX")
+        A.check(k, o[k], ref, rows if per_row else None)
+        if per_row and outside.any():           # as they were
+            assert bool((o[k].cpu()[outside] == o[k].new_full((1,), SENTINEL).cpu()).all()), k
+
+
+CASES = [
+    # T, J, D, n, R, S, single, first, behind
+    (1, 64, 64, 1, 1, 1, True, 0, 0),
+    (1, 1000, 520, 4, 16, 1, True, 0, 0),
+    (5, 72, 8, 3, 8, 5, True, 0, 0),
+    (33, 8, 136, 2, 17, 3, False, 0, 0),
+    (64, 1032, 264, 20, 16, 64, True, 0, 0),
+    (70, 264, 1032, 20, 33, 60, True, 3, 7),
+    (129, 136, 200, 5, 64, 9, False, 0, 0),
+    (257, 520, 328, 3, 40, 2, False, 1, 0),
+    (300, 256, 512, 2, 256, 6, False, 0, 20),
+    (515, 392, 72, 7, 100, 130, False, 0, 3),
+    (700, 128, 640, 40, 5, 200, False, 0, 0),
+    (1100, 520, 264, 1, 12, 1, False, 0, 0),
+]
+
+
+@pytest.mark.parametrize("case", CASES)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_forward_and_backward(ctx, case, dtype):
+    T, J, D, n, R, S, single, first, behind = case
+    print("adapter", case, dtype, flush=True)
+    c = A.poison(A.make(T, J, D, n, R, S, dtype, seed=T + R, single=single, first=first, behind=behind))
+    d, o = to_dev(c), outputs(c)
+    forward(ctx, d, o)
+    backward(ctx, d, o)                       # projections computed again
+    compare(c, o)
+    p = outputs(c)
+    p["H"] = o["H"]
+    p["H"][torch.isnan(p["H"])] = 0
+    backward(ctx, d, p, H=p["H"])             # and the forward call's taken
+    compare(c, p, ("dX", "dU", "dV"))
+    q = outputs(c)
+    forward(ctx, d, q, H=False)
+    assert torch.equal(q["Y"], o["Y"])
+    assert bool((q["H"] == SENTINEL).all())
+
+
+@pytest.mark.parametrize("J,D,n,R", [(1003, 2047, 2, 12), (65, 63, 3, 5), (2, 3, 2, 1), (130, 1, 1, 7)])
+def test_fp32_odd_sizes(ctx, J, D, n, R):
+    c = A.poison(A.make(90, J, D, n, R, 4, F32, seed=J, behind=2))
+    d, o = to_dev(c), outputs(c)
+    forward(ctx, d, o)
+    backward(ctx, d, o)
+    compare(c, o)
+
+
+@pytest.mark.parametrize("T,J,D,n,R,S", [(0, 64, 64, 2, 4, 0), (9, 64, 64, 2, 4, 0), (9, 64, 72, 0, 4, 3), (40, 64, 64, 3, 4, 8)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_nothing_there(ctx, T, J, D, n, R, S, dtype):
+    """No rows, no requests, no blocks, blocks of rank 0: outputs of rows that belong to requests are the shared matrix's alone,
+    gradients zeros."""
+    c = A.make(T, J, D, n, R, S, dtype, seed=1)
+    if S == 8:
+        c["ranks"][:] = 0
+    if S == 0:
+        c["start"] = torch.tensor([T])
+    A.poison(c)
+    d, o = to_dev(c), outputs(c)
+    forward(ctx, d, o)
+    backward(ctx, d, o)
+    compare(c, o)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_numbers_out_of_range(ctx, dtype):
+    """Blocks outside the pool are none, ranks are clamped; no ranks and no scale: all pairs, 1."""
+    c = A.make(60, 72, 136, 3, 9, 6, dtype, seed=4, none=0)
+    c["adapter"] = torch.tensor([5, 0, -7, 3, 2, 1], dtype=torch.int32)
+    c["ranks"] = torch.tensor([99, -4, 9], dtype=torch.int32)
+    d, o = to_dev(c), outputs(c)
+    forward(ctx, d, o)
+    backward(ctx, d, o)
+    compare(c, o)
+    c["ranks"][:], c["scale"][:] = 9, 1.0
+    d, o = to_dev(c), outputs(c)
+    d["ranks"] = d["scale"] = None
+    forward(ctx, d, o)
+    backward(ctx, d, o)
+    compare(c, o)
+
+
+@pytest.mark.parametrize("layout", ["copy", "planes"])
+@pytest.mark.parametrize("T,J,D", [(3, 520, 200), (150, 264, 328), (400, 1000, 72)])
+def test_attached_matrix(sfb, layout, T, J, D):
+    """bf16 blocks beside the fp32 matrix that a context keeps a bf16 copy or two planes of."""
+    c = A.make(T, J, D, 3, 16, 3, BF16, seed=8)
+    W = torch.randn(J, D, generator=torch.Generator().manual_seed(2)) * D ** -0.5
+    own = sfb.Context(0)
+    Wd = W.to("cuda:0")
+    (own.sfb_shadow_attach if layout == "copy" else own.sfb_split_attach)(Wd)
+    # (the planes' high halves round ties away from zero)
+    c["W"] = W.to(BF16) if layout == "copy" else ((W.view(torch.int32) + 0x8000) >> 16).to(torch.int16).view(BF16)
+    d, o = to_dev(c), outputs(c)
+    forward(own, d, o, W=Wd)
+    backward(own, d, o, W=Wd)
+    compare(c, o)
+    own.close()
+
+
+def test_block_is_what_apply_would_make(ctx, sfb):
+    """W + scale U^T V by sfb_apply, and the projection with it, against the block beside W."""
+    T, J, D, R = 65, 264, 520, 12
+    c = A.make(T, J, D, 1, R, 1, F32, seed=5, none=0)
+    c["adapter"][:] = 0
+    d, o = to_dev(c), outputs(c)
+    forward(ctx, d, o)
+    merged = d["W"].clone()
+    s = float(c["scale"][0])
+    ctx.sfb_apply(merged, d["U"][0].contiguous(), d["V"][0].contiguous(), -s)
+    plain = outputs(c)
+    ctx.sfb_adapter_forward(merged, d["X"], d["start"], torch.full_like(d["adapter"], -1), d["U"], d["V"], plain["Y"])
+    ref, _ = A.reference(c)
+    # both are within the fp32 bound of the exact value; the merged matrix is rounded once more (2^-24 of each element)
+    extra = 2.0 ** -24 * (np.abs(c["X"].double().numpy()) @ np.abs(merged.cpu().double().numpy()).T)
+    assert np.all(np.abs((plain["Y"] - o["Y"]).cpu().double().numpy()) <= 2 * ref["Y_tol"] + extra + 2.0 ** -22 * np.abs(ref["Y"]))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,S", [(24, 24), (300, 12)])
+def test_what_is_not_finite_stays_in_its_row(ctx, dtype, T, S):
+    """Infinities and not-a-numbers in one request's rows or block do not reach the rows of others."""
+    J, D, n, R = 136, 200, 4, 8
+    c = A.make(T, J, D, n, R, S, dtype, seed=11, single=S == T, none=0)
+    c["ranks"][:] = R
+    c["adapter"] = (torch.arange(S) % n).to(torch.int32)
+    ref, rows = A.reference(c)
+    bad = [t for t in range(T) if int(c["adapter"][max(q for q in range(S) if int(c["start"][q]) <= t)]) == 1]
+    good = sorted(set(rows) - set(bad))
+    c["U"][1, 2, 5] = float("inf")
+    c["V"][1, 3, 7] = float("nan")
+    d, o = to_dev(c), outputs(c)
+    forward(ctx, d, o)
+    backward(ctx, d, o)
+    for k in ("Y", "dX"):
+        A.check(k, o[k], ref, good)
+    others = [0, 2, 3]
+    for k in ("dU", "dV"):
+        got = {k: torch.tensor(0)}
+        A.check(k, o[k][others], {k: ref[k][others], k + "_tol": ref[k + "_tol"][others]})
+    assert bool(torch.isnan(o["Y"][bad].float()).any())
+    # an infinity in a factor is an infinity of the sum, not a not-a-number
+    c = A.make(T, J, D, n, R, S, dtype, seed=12, single=S == T, none=0)
+    c["ranks"][:] = R
+    c["U"][:, 2, 5] = float("inf")
+    d, o = to_dev(c), outputs(c)
+    forward(ctx, d, o)
+    h = o["H"].cpu()
+    assert bool((torch.isinf(o["Y"].cpu()[:, 5].float()) | (h[:, 2] == 0)).all())
+    assert bool((torch.sign(o["Y"].cpu()[:, 5].float()) == torch.sign(h[:, 2])).all())
+
+
+def test_gradients_against_differences(ctx):
+    """d/ds of sum(Y * G) along random directions of X, U and V, by central differences of the forward call in fp32."""
+    T, J, D, n, R, S = 40, 48, 56, 3, 6, 5
+    c = A.make(T, J, D, n, R, S, F32, seed=21)
+    d, o = to_dev(c), outputs(c)
+    forward(ctx, d, o)
+    backward(ctx, d, o)
+    g = torch.Generator(device="cuda:0").manual_seed(3)
+    for name, grad in (("X", "dX"), ("U", "dU"), ("V", "dV")):
+        step = torch.randn(d[name].shape, generator=g, device="cuda:0")
+        loss = []
+        for sign in (1, -1):
+            e = dict(d)
+            e[name] = d[name] + sign * 2.0 ** -4 * step
+            p = outputs(c)
+            forward(ctx, e, p)
+            loss.append((p["Y"].double() * d["dY"].double()).sum().item())
+        # Y is linear in each of them alone: the difference is exact but for the two sums' rounding
+        got, want = (o[grad].double() * step.double()).sum().item(), (loss[0] - loss[1]) * 2.0 ** 3
+        ref, _ = A.reference(c)
+        room = 2.0 ** 5 * float((ref["Y_tol"] * 4 * np.abs(c["dY"].double().numpy())).sum())
+        assert abs(got - want) <= room + 1e-4 * abs(want), (name, got, want, room)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,S,single", [(16, 16, True), (300, 6, False)])
+def test_graph_replays_other_batches(sfb, dtype, T, S, single):
+    """One captured forward and backward serves batches of other compositions; a second graph and eager calls in between."""
+    J, D, n, R = 264, 328, 4, 16
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ctx = sfb.Context(0)
+        c = A.make(T, J, D, n, R, S, dtype, seed=31, single=single)
+        d, o = to_dev(c), outputs(c)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            forward(ctx, d, o)
+            backward(ctx, d, o, H=o["H"])
+        big = A.make(4 * T, J, D, n, R, 3, dtype, seed=32)          # the workspace grows after the capture
+        db, ob = to_dev(big), outputs(big)
+        forward(ctx, db, ob)
+        side.synchronize()
+        for k in range(4):
+            other = A.make(T, J, D, n, R, S, dtype, seed=40 + k, single=single, behind=0 if single else k)
+            for key in KEYS:
+                d[key].copy_(other[key].to("cuda:0"))
+            for key in o:
+                o[key].fill_(SENTINEL)
+            graph.replay()
+            side.synchronize()
+            got = {key: v.clone() for key, v in o.items()}
+            compare(other, got)
+            e = outputs(other)
+            forward(ctx, d, e)
+            backward(ctx, d, e, H=e["H"])
+            forward(ctx, db, ob)
+            side.synchronize()
+            for key in o:
+                assert torch.equal(e[key], got[key]), key          # the same bits
+    ctx.close()
+
+
+def test_wrong_arguments(sfb, ctx):
+    c = A.make(20, 64, 72, 2, 8, 3, BF16, seed=1)
+    d, o = to_dev(c), outputs(c)
+    for key, bad in (("X", d["X"][:, :64]), ("X", d["X"].float()), ("U", d["U"].float()), ("start", d["start"].int()),
+                     ("start", d["start"][:-1]), ("adapter", d["adapter"].long()), ("ranks", d["ranks"][:1]),
+                     ("scale", d["scale"].double()), ("W", d["W"].t())):
+        e = dict(d)
+        e[key] = bad
+        with pytest.raises((TypeError, ValueError)):
+            forward(ctx, e, o)
+    with pytest.raises(sfb.SfbError) as err:          # an fp32 matrix that is not attached, beside bf16 blocks
+        forward(ctx, d, o, W=d["W"].float())
+    assert err.value.code == sfb.SFB_EINVAL
+    with pytest.raises((TypeError, ValueError)):
+        forward(ctx, d, dict(o, Y=o["Y"][:10]))
+    with pytest.raises((TypeError, ValueError)):
+        backward(ctx, d, dict(o, dU=o["dU"].to(BF16)))
+    with pytest.raises(sfb.SfbError):                 # one of the two gradients
+        ctx.sfb_adapter_backward(d["W"], d["X"], d["dY"], d["start"], d["adapter"], d["U"], d["V"], dU=o["dU"])
+    torch.cuda.synchronize()
+    assert bool((o["Y"] == o["Y"].new_full((1,), SENTINEL)).all())
+
+
+def test_large_offsets(ctx):
+    """Buffers of more than 2^31 elements: the last rows of X and the last blocks of the pool."""
+    T, J, D, n, R = 70000, 64, 32768, 1100, 64
+    X = torch.zeros(T, D, dtype=BF16, device="cuda:0")
+    V = torch.zeros(n, R, D, dtype=BF16, device="cuda:0")
+    U = torch.zeros(n, R, J, dtype=BF16, device="cuda:0")
+    W = torch.zeros(J, D, dtype=BF16, device="cuda:0")
+    X[-1, -8:], V[-1, :, -4:], U[-1], W[:, -2:] = 1.0, 0.5, 0.25, 2.0
+    start = torch.tensor([T - 40, T - 3, T], device="cuda:0")
+    adapter = torch.tensor([0, n - 1], dtype=torch.int32, device="cuda:0")
+    Y = torch.zeros(T, J, dtype=BF16, device="cuda:0")
+    ctx.sfb_adapter_forward(W, X, start, adapter, U, V, Y)
+    torch.cuda.synchronize()
+    want = torch.zeros(3, J)
+    want[-1] = 4.0 + 64 * 2.0 * 0.25
+    assert torch.equal(Y[-3:].float().cpu(), want)
+    assert float(Y[:-3].float().abs().max()) == 0.0
+    del X, V, U, W, Y
+    torch.cuda.empty_cache()

@@ -1,0 +1,159 @@
+"""Norm and clipping of a list of tensors against 64-bit sums: empty and odd sizes, unaligned tensors, many of them, both
+types, values whose squares leave fp32, not-finite ones; in place and into other tensors."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def sfb():
+    import paper_1409_5705_amd as m
+    m.lib()
+    return m
+
+
+@pytest.fixture(scope="module")
+def ctx(sfb):
+    c = sfb.Context(0)
+    yield c
+    c.close()
+
+
+def tensors(sizes, seed, bf16=lambda k: k % 3 == 1, offset=lambda k: 0):
+    g = torch.Generator(device="cuda:0").manual_seed(seed)
+    out = []
+    for k, n in enumerate(sizes):
+        dt = BF16 if bf16(k) else F32
+        base = torch.randn(n + offset(k), generator=g, device="cuda:0").to(dt)
+        out.append(base[offset(k):])
+    return out
+
+
+def norm64(ts):
+    return math.sqrt(sum(float(t.double().square().sum()) for t in ts))
+
+
+def check_clipped(src, dst, coef):
+    for s, d in zip(src, dst):
+        want = s.double() * coef
+        half_step = 2.0 ** -8 if s.dtype == BF16 else 2.0 ** -24
+        # the scale itself is rounded to fp32, and the product of fp32 values
+        assert bool(((d.double() - want).abs() <= want.abs() * (half_step + 2.0 ** -23) + 1e-40).all())
+
+
+LISTS = [
+    ([1], lambda k: 0),
+    ([0, 5, 0], lambda k: 0),
+    ([7, 8, 9, 4095, 4096, 4097, 20001], lambda k: 0),
+    ([13, 1000, 4099, 70001], lambda k: 1 + k % 3),
+    ([3 + 17 * k for k in range(300)], lambda k: k % 2),
+    ([5_000_003, 17, 1_234_567, 64], lambda k: 0),
+    ([1] * 1500, lambda k: 0),
+]
+
+
+@pytest.mark.parametrize("which", range(len(LISTS)))
+def test_norm_and_clip(sfb, ctx, which):
+    sizes, offset = LISTS[which]
+    print("clip", which, flush=True)
+    src = tensors(sizes, which, offset=offset)
+    before = [t.clone() for t in src]
+    dst = [torch.full_like(t, 7.0) for t in src]
+    norm = torch.full((1,), -1.0, device="cuda:0")
+    want = norm64(src)
+    ctx.sfb_grad_norm(sfb.TensorList(src), norm)
+    assert abs(norm.item() - want) <= 2.0 ** -24 * want * 1.001
+    for bound in (0.0, 0.25 * want, want * 2, float("inf")):
+        norm.fill_(-1.0)
+        ctx.sfb_clip_grads(sfb.TensorList(src, dst), bound, norm)
+        assert abs(norm.item() - want) <= 2.0 ** -24 * want * 1.001
+        check_clipped(before, dst, min(1.0, bound / want) if want > 0 else 1.0)
+        assert all(torch.equal(a, b) for a, b in zip(src, before))
+        if want < bound:
+            assert all(torch.equal(a, b) for a, b in zip(dst, before))
+    lst = sfb.TensorList(src)
+    ctx.sfb_clip_grads(lst, want * 2, norm)                 # within the bound: left alone
+    assert all(torch.equal(a, b) for a, b in zip(src, before))
+    ctx.sfb_clip_grads(lst, 0.5 * want, norm)
+    check_clipped(before, src, 0.5)
+    again = norm.clone()
+    for s, b in zip(src, before):
+        s.copy_(b)
+    ctx.sfb_clip_grads(lst, 0.5 * want, norm)
+    assert torch.equal(again, norm)
+
+
+def test_empty_list(sfb, ctx):
+    norm = torch.full((1,), -1.0, device="cuda:0")
+    ctx.sfb_grad_norm(sfb.TensorList([]), norm)
+    assert norm.item() == 0.0
+    ctx.sfb_clip_grads(sfb.TensorList([torch.empty(0, device="cuda:0")]), 1.0, norm.fill_(-1.0))
+    assert norm.item() == 0.0
+
+
+@pytest.mark.parametrize("value", [3e38, 1e30, 1e-30, 1e-44])
+def test_squares_outside_fp32(sfb, ctx, value):
+    t = torch.full((1000,), value, device="cuda:0")
+    want = norm64([t])
+    norm = torch.zeros(1, device="cuda:0")
+    out = torch.zeros_like(t)
+    ctx.sfb_clip_grads(sfb.TensorList([t], [out]), 1.0, norm)
+    if want < torch.finfo(F32).max:
+        assert abs(norm.item() - want) <= 2.0 ** -24 * want + 1.5e-45
+    else:
+        assert math.isinf(norm.item())                      # beyond fp32, and still clipped to 1
+    check_clipped([t], [out], min(1.0, 1.0 / want))
+    if want > 1:
+        assert abs(norm64([out]) - 1.0) < 1e-5
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("at", [0, 1, 4999])
+def test_not_finite(sfb, ctx, bad, at):
+    a, b = torch.ones(5000, device="cuda:0"), torch.ones(5000, device="cuda:0", dtype=BF16)
+    (a if at != 1 else b)[at] = bad
+    norm = torch.zeros(1, device="cuda:0")
+    ctx.sfb_clip_grads(sfb.TensorList([a, b]), 1.0, norm)
+    assert norm.item() == bad or (math.isnan(bad) and math.isnan(norm.item()))
+    rest = torch.ones(5000, dtype=torch.bool, device="cuda:0")
+    rest[at] = False
+    for t in (a, b):
+        assert bool((t[rest] == 0).all() if math.isinf(bad) else torch.isnan(t).all())
+
+
+def test_more_than_2_31_elements(sfb, ctx):
+    n = (1 << 31) + 5
+    t = torch.zeros(n, device="cuda:0", dtype=BF16)
+    t[-1], t[0] = 3.0, 4.0
+    norm = torch.zeros(1, device="cuda:0")
+    ctx.sfb_clip_grads(sfb.TensorList([t]), 1.0, norm)
+    assert norm.item() == 5.0
+    assert abs(t[-1].item() - 0.6) <= 0.6 * 2.0 ** -8 and abs(t[0].item() - 0.8) <= 0.8 * 2.0 ** -8
+    del t
+    torch.cuda.empty_cache()
+
+
+def test_wrong_arguments(sfb, ctx):
+    a = torch.ones(10, device="cuda:0")
+    norm = torch.zeros(1, device="cuda:0")
+    with pytest.raises(TypeError):
+        sfb.TensorList([a.double()])
+    with pytest.raises(TypeError):
+        sfb.TensorList([torch.ones(3)])
+    with pytest.raises(ValueError):
+        sfb.TensorList([torch.ones(4, 4, device="cuda:0").t()])
+    with pytest.raises(ValueError):
+        sfb.TensorList([a], [a, a])
+    with pytest.raises((TypeError, ValueError)):
+        sfb.TensorList([a], [a.to(BF16)])
+    for bound in (-1.0, float("nan")):
+        with pytest.raises(sfb.SfbError) as e:
+            ctx.sfb_clip_grads(sfb.TensorList([a]), bound, norm)
+        assert e.value.code == sfb.SFB_EINVAL
+    with pytest.raises((TypeError, ValueError)):
+        ctx.sfb_grad_norm(sfb.TensorList([a]), norm.double())
+    assert bool((a == 1).all())
