@@ -84,10 +84,10 @@ struct AdapterOuterArgs {
 };
 hipError_t launch_adapter_outer(const AdapterOuterArgs& a, hipStream_t stream);
 
-// Norm over the tensors of a list and their scaling.  partial: grad_norm_partials(...) + 1 doubles.
+// Norm over the tensors of a list and their scaling.  partial: grad_norm_partials(...) + 1 doubles.  Where launch_clip follows
+// (clip), with the same list and `partial`, it may be that which writes *norm.
 int64_t grad_norm_partials(const sfb_tensor* list, int64_t count);
-hipError_t launch_grad_norm(const sfb_tensor* list, int64_t count, double* partial, float* norm, hipStream_t stream);
-// (after launch_grad_norm on the same list and `partial`)
-hipError_t launch_clip(const sfb_tensor* list, int64_t count, const double* partial, double max_norm, hipStream_t stream);
+hipError_t launch_grad_norm(const sfb_tensor* list, int64_t count, double* partial, float* norm, bool clip, hipStream_t stream);
+hipError_t launch_clip(const sfb_tensor* list, int64_t count, const double* partial, double max_norm, float* norm, hipStream_t stream);
 
 }  // namespace sfb

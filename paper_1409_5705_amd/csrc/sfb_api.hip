@@ -1255,8 +1255,8 @@ static int grad_norm_impl(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, b
     const DeviceScope scope(ctx->device);
     SFB_TRY(scope.status);
     double* partial = reinterpret_cast<double*>(ctx->ws);
-    SFB_RUN(KID_GRAD_NORM, sfb::launch_grad_norm(list, count, partial, norm, ctx->stream));
-    if (clip) SFB_RUN(KID_CLIP, sfb::launch_clip(list, count, partial, (double)max_norm, ctx->stream));
+    SFB_RUN(KID_GRAD_NORM, sfb::launch_grad_norm(list, count, partial, norm, clip, ctx->stream));
+    if (clip) SFB_RUN(KID_CLIP, sfb::launch_clip(list, count, partial, (double)max_norm, norm, ctx->stream));
     return SFB_OK;
 }
 
