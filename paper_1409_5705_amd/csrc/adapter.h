@@ -34,11 +34,14 @@ struct AdapterProjectArgs {
     int32_t* row_adapter;
     float* H;
     float* H_out;
+    uint16_t* Hx;              // nullable: [T][2 adapter_pitch(rank)]: H in two bf16 terms, the 16 first and then the 16 second ones
+                               // of every 16 pairs
 };
 hipError_t launch_adapter_project(const AdapterProjectArgs& a, DeviceInfo& dev, hipStream_t stream);
 
-// base[s][m][n] = sum over the s-th part of k of A[m][k] B(n, k); A bf16 [M][K] row-major; B(n, k) = W[n][k] or, transposed,
-// W[k][n], with W [rows][cols] bf16 row-major or a bf16 operand in blocks of 256 x 64 (pitch: its zero-padded columns).
+// A bf16 [M][K] row-major times B(n, k) = W[n][k] or, transposed, W[k][n], with W [rows][cols] bf16 row-major or a bf16 operand
+// in blocks of 256 x 64.  split 1: out[t][n] = sum_k A[t][k] B(n, k) + sum_r H[t][r] F_a[r][n] for the rows of requests (H and Hx:
+// launch_adapter_project's).  More: planes[s][t][n], the s-th part of the first sum alone, for launch_adapter_join.
 struct AdapterBase {
     const uint16_t* A;
     const uint16_t* W;
@@ -46,6 +49,13 @@ struct AdapterBase {
     int64_t M, N, K;
     float* planes;             // [split][M][N]
     int split;
+    uint16_t* out;
+    const int32_t* row_adapter;
+    const uint16_t* Hx;
+    const float* H;
+    const uint16_t* F;
+    const int32_t* ranks;
+    int rank;
 };
 hipError_t launch_adapter_base_bf16(const AdapterBase& a, DeviceInfo& dev, hipStream_t stream);
 int adapter_base_split(int64_t M, int64_t N, int64_t K);

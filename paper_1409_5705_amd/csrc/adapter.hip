@@ -79,8 +79,21 @@ struct ProjectParams {
     int32_t* row_adapter;
     float* H;
     float* H_out;
+    uint16_t* Hx;
     int pitch;
 };
+
+// Two bf16 terms of a value: its upper half and what is left, rounded (together off by at most 2^-17 of the value, and of its
+// sign); one that is not finite as itself twice.
+__device__ __forceinline__ void two_terms(float v, uint16_t& first, uint16_t& second)
+{
+    const uint32_t bits = __float_as_uint(v);
+    const bool finite = (~bits & 0x7f800000u) != 0;
+    first = (uint16_t)(finite ? bits >> 16 : pack_bf16(v, 0.f));
+    second = (uint16_t)pack_bf16(finite ? v - __uint_as_float(bits & 0xffff0000u) : v, 0.f);
+}
+// Place of pair r's first term in a row of the two-term array; the second one is 16 further.
+__device__ __forceinline__ int term_at(int r) { return (r >> 4) * 32 + (r & 15); }
 
 constexpr int64_t MAX_BLOCKS = 1 << 22;      // workgroups of a launch (threads of a grid are counted in 32 bits)
 constexpr int PW = 8;      // wavefronts that share k
@@ -118,6 +131,7 @@ __global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams 
         const int t = i / (16 * RT), r = r0 + i % (16 * RT);
         if (row_of[t] < 0 && r < p.pitch) {
             p.H[(t0 + t) * p.pitch + r] = 0.f;
+            if (p.Hx) p.Hx[(t0 + t) * 2 * p.pitch + term_at(r)] = p.Hx[(t0 + t) * 2 * p.pitch + term_at(r) + 16] = 0;
             if (p.H_out && row_of[t] == ROW_NONE && r < rows.rank) p.H_out[(t0 + t) * rows.rank + r] = 0.f;
         }
     }
@@ -173,7 +187,13 @@ __global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float h = r + i < rank ? s * sum[i] : 0.f;
-                    if (r + i < p.pitch) p.H[(t0 + t) * p.pitch + r + i] = h;
+                    if (r + i < p.pitch) {
+                        p.H[(t0 + t) * p.pitch + r + i] = h;
+                        if (p.Hx) {
+                            uint16_t* const at = p.Hx + (t0 + t) * 2 * p.pitch + term_at(r + i);
+                            two_terms(h, at[0], at[16]);
+                        }
+                    }
                     if (p.H_out && r + i < rows.rank) p.H_out[(t0 + t) * rows.rank + r + i] = h;
                 }
             }
@@ -401,7 +421,7 @@ hipError_t outer_rank(const OuterParams& p, hipStream_t stream)
 hipError_t launch_adapter_project(const AdapterProjectArgs& a, DeviceInfo&, hipStream_t stream)
 {
     if (a.rows.T <= 0) return hipSuccess;
-    ProjectParams p = {a.rows, a.X, a.F, a.K, a.row_adapter, a.H, a.H_out, adapter_pitch(a.rows.rank)};
+    ProjectParams p = {a.rows, a.X, a.F, a.K, a.row_adapter, a.H, a.H_out, a.Hx, adapter_pitch(a.rows.rank)};
     // A tile of rows is gone through once for every block in it: rows of requests of a few tokens go one by one.
     const int rows = a.rows.requests * 8 > a.rows.T ? 1 : 32;
     if (a.bf16) return project_rank<uint16_t, true>(p, rows, stream);

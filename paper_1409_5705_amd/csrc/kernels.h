@@ -15,6 +15,7 @@ struct DeviceInfo {
     bool gemm_f32x3_lds_set[10] = {};                     // of the kernel on three bf16 terms (operand combination x tile shape)
     bool apply_gather_lds_set[2] = {};                   // of the apply of sparse factors (fp32 array, planes)
     bool fwd_stream_lds_set[6] = {};                     // and of the streaming bf16 forward
+    bool adapter_base_lds_set[8] = {};                   // and of the product beside the factor blocks (tile, orientation, split)
     int softmax_wait_polls = 1000;                 // bound of the one-read softmax's wait for a partner's word
 };
 

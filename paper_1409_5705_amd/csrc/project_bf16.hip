@@ -1,14 +1,25 @@
-// The product of bf16 rows with a shared bf16 matrix as it lies in memory, for the calls with factor blocks beside it:
+// The product of bf16 rows with a shared bf16 matrix as it lies in memory, and the factor blocks' part of it:
 //
-//   forward   base[t][j] = sum_d X[t][d] W[j][d]         both operands contiguous along k
-//   backward  base[t][d] = sum_j dY[t][j] W[j][d]        W contiguous along the output's columns
+//   forward   out[t][j] = sum_d X[t][d] W[j][d]  + sum_r H[t][r] U_a[r][j]       W contiguous along k
+//   backward  out[t][d] = sum_j dY[t][j] W[j][d] + sum_r dH[t][r] V_a[r][d]      W contiguous along the output's columns
 //
 // Neither operand is copied or transposed first.  Tiles go from memory straight into LDS through buffer descriptors, whose
 // range check fills what lies behind the last row, column or k with zeros.  In the backward W's tile lies in LDS as 64 rows
-// (k) of BN columns, and the matrix operand is read with the transposing LDS read (four rows of 16 columns a group of 16
-// lanes; lane i gets column i).
+// (k) of TBN columns and is read with the transposing LDS read (four rows of 16 columns a group of 16 lanes; lane i gets
+// column i); so are the blocks' factors in both.
 // W is the first operand of the MFMA, so a lane's results are one row of the output, and the columns are dealt to the MFMA
-// tiles such that a lane owns runs of eight consecutive ones and the four lanes of a row 32 of them.
+// tiles such that a lane owns runs of eight consecutive ones and the four lanes of a row 32 of them: 16-byte stores, 64 bytes
+// of a row together.
+//
+// The blocks' part comes first and is what the accumulators start from.  H is held as two bf16 terms side by side along k
+// against the same factors: 16 pairs are one MFMA of k = 32.  Per block that occurs in a tile its factors are loaded and
+// multiplied with the rows that use it; the others' H counts as zeros there.  A factor that is not finite must not meet those
+// zeros: it counts as zero too, and the rows that use it get its products when they are stored.
+//
+// The matrix pipes bound it where there are tiles enough: 8192 rows, 4096 x 4096 in 219 to 242 us forward (1.2 PFLOP/s) and 193
+// us backward (1.4 PFLOP/s).  What a tile costs besides its k-loop is instructions that are executed once, so their number
+// counts, and a register that is spilled around them more so (an earlier form with scratch memory and 80 KB of code: 30 us a
+// tile, this one 8).
 #include "adapter.h"
 #include "planes.h"
 
@@ -18,195 +29,488 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 struct BaseParams {
     const uint16_t* A;
     const uint16_t* W;
     int64_t M, N, K, ldw;
     int64_t pitch;             // blocked W: columns of the operand; 0: rows of ldw
-    float* planes;
+    float* planes;             // split: [split][M][N]
     int split;
+    uint16_t* out;             // not split: [M][N]
+    const int32_t* row_adapter;
+    const uint16_t* Hx;        // [M][2 adapter_pitch(rank)]
+    const float* H;            // [M][adapter_pitch(rank)]
+    const uint16_t* F;         // [count][rank][N]
+    const int32_t* ranks;
+    int rank;
     int tiles_m, tiles_n, group_m, num_xcd;
 };
 
 constexpr uint32_t OUT_OF_RANGE = 0x80000000u;
 
 // A buffer descriptor of 2 GiB from base on (raw bytes; reads beyond it give zeros).
-__device__ __forceinline__ u32x4 descriptor(uint64_t base)
+__device__ __forceinline__ u32x4 descriptor(uint64_t at)
 {
-    const uint64_t b = uniform64(base);
-    return u32x4{(uint32_t)b, (uint32_t)(b >> 32), OUT_OF_RANGE, 0x00020000u};
+    const uint64_t base = uniform64(at);
+    return u32x4{(uint32_t)base, (uint32_t)(base >> 32), OUT_OF_RANGE, 0x00020000u};
 }
+template <uint32_t OFF>
 __device__ __forceinline__ void buffer_to_lds_16(uint32_t lds_addr, u32x4 rsrc, uint32_t voff)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_addr), "v"(voff), "s"(rsrc) : "memory");
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_addr), "v"(voff), "s"(rsrc), "n"(OFF)
+                 : "memory", "scc");
+}
+
+// The accumulators stay in the accumulation registers: left to itself the compiler moves them to ordinary ones, all at once,
+// for any arithmetic on them, and spills.  The caller sees to it that the MFMAs that wrote them have retired.
+__device__ __forceinline__ float acc_read(float element)
+{
+    float v;
+    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(element));
+    return v;
+}
+// More wait states than the longest MFMA needs to write back its result.
+__device__ __forceinline__ void mfma_settle() { asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory"); }
+
+// The same value, and nothing that the compiler can work out ahead of time from it: what is needed once a tile is not to be
+// kept in registers over the k-loop.
+__device__ __forceinline__ int here(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+__device__ __forceinline__ int here_scalar(int v)
+{
+    asm volatile("" : "+s"(v));
+    return v;
 }
 
 // Column of the output's tile that row i of MFMA tile tb of a wavefront holds.
-__device__ __forceinline__ int column_of(int tb, int i) { return 32 * (tb >> 1) + 8 * (i >> 2) + 4 * (tb & 1) + (i & 3); }
+__device__ __forceinline__ constexpr int column_of(int tb, int i) { return 32 * (tb >> 1) + 8 * (i >> 2) + 4 * (tb & 1) + (i & 3); }
 
-// Tiles of 32 TM rows x 32 TN columns, 2 x 2 wavefronts of 16 TM x 16 TN.
-template <int TM, int TN, bool TRANSPOSED>
-__global__ __launch_bounds__(256) void adapter_base_kernel(BaseParams p)
+// The i-th of n things goes after MFMA (2 i + 1) m / (2 n) of the m MFMAs of a window; how many go after MFMA j, and which first.
+constexpr int first_slot(int j, int n, int m)
 {
-    constexpr int TBM = 32 * TM, TBN = 32 * TN;
+    for (int i = 0; i < n; ++i)
+        if ((2 * i + 1) * m / (2 * n) >= j) return i;
+    return n;
+}
+
+// Tiles of 32 TM rows x 32 TN columns, 2 x 2 wavefronts of 16 TM x 16 TN.  Workgroups are persistent (one or two a CU); two
+// LDS stages of a k-slice (64) each.  The loads of slice s + 2 go out once every wavefront has read the last fragments of slice
+// s, spread between the MFMAs of its second k-step; fragments are double-buffered in registers across the barriers.
+template <int TM, int TN, bool TRANSPOSED, bool SPLIT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1 : 2, TM == 8 ? 1 : 2))) void adapter_base_kernel(BaseParams p)
+{
+    constexpr int TBM = 32 * TM, TBN = 32 * TN, STEP = TM * TN;
     constexpr uint32_t A_BYTES = TBM * 128, STAGE_BYTES = A_BYTES + TBN * 128;
+    constexpr uint32_t F_CHUNK = 16 * TBN * 2, F_OFF = 2 * STAGE_BYTES;
+    constexpr int LOADS = TM + TN, BPOS = STEP / 2, N2B = LOADS / 2, N3 = LOADS - N2B;
+    constexpr int READS = TM + (TRANSPOSED ? 2 : 1) * TN;
     extern __shared__ u32x4 smem[];
     char* const lds = reinterpret_cast<char*>(smem);
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave0 = __builtin_amdgcn_readfirstlane(tid >> 6), wave = wave0;
     const int wm0 = (wave >> 1) * 16 * TM, wn0 = (wave & 1) * 16 * TN;
 
-    // each XCD a contiguous range of a raster of groups of group_m row-tiles, row-tile index fastest
-    int64_t m0, n0;
-    {
-        const uint32_t tiles = gridDim.x, xcds = (uint32_t)p.num_xcd, tiles_n = (uint32_t)p.tiles_n, tiles_m = (uint32_t)p.tiles_m;
-        const uint32_t x = blockIdx.x % xcds, wi = blockIdx.x / xcds, q = tiles / xcds, r = tiles % xcds;
-        const uint32_t t = x * q + (x < r ? x : r) + wi;
-        const uint32_t per_group = (uint32_t)p.group_m * tiles_n;
+    // ---- persistent schedule: each XCD a contiguous range of a raster of groups of group_m row-tiles, row-tile index fastest
+    const uint32_t tiles = (uint32_t)p.tiles_m * (uint32_t)p.tiles_n;
+    const uint32_t xcds = (uint32_t)p.num_xcd, xcd = blockIdx.x % xcds, wi = blockIdx.x / xcds;
+    const uint32_t per_xcd = gridDim.x / xcds + (xcd < gridDim.x % xcds ? 1 : 0);      // workgroups of this XCD
+    const uint32_t xcd_start = xcd * (tiles / xcds) + (xcd < tiles % xcds ? xcd : tiles % xcds);
+    const uint32_t xcd_count = tiles / xcds + (xcd < tiles % xcds ? 1 : 0);
+    if (wi >= xcd_count) return;
+    const int n_my = (int)((xcd_count - wi + per_xcd - 1) / per_xcd);
+    auto tile_origin = [&](int ordinal, int64_t& m0, int64_t& n0) {
+        const uint32_t t = xcd_start + (uint32_t)ordinal * per_xcd + wi;
+        const uint32_t per_group = (uint32_t)p.group_m * (uint32_t)p.tiles_n;
         const uint32_t grp = t / per_group, rr = t % per_group, first = grp * (uint32_t)p.group_m;
-        const uint32_t gm = tiles_m - first < (uint32_t)p.group_m ? tiles_m - first : (uint32_t)p.group_m;
+        const uint32_t gm = (uint32_t)p.tiles_m - first < (uint32_t)p.group_m ? (uint32_t)p.tiles_m - first : (uint32_t)p.group_m;
         m0 = (int64_t)(first + rr % gm) * TBM;
         n0 = (int64_t)(rr / gm) * TBN;
-    }
-    const int64_t slices = (p.K + BK - 1) / BK;
-    const int64_t s_begin = slices * blockIdx.y / p.split, s_end = slices * (blockIdx.y + 1) / p.split;
-    const int nk = (int)(s_end - s_begin);
+    };
+    const int slices = (int)((p.K + BK - 1) / BK);
+    const int s_begin = SPLIT ? (int)((int64_t)slices * blockIdx.y / p.split) : 0;
+    const int nk = (SPLIT ? (int)((int64_t)slices * (blockIdx.y + 1) / p.split) : slices) - s_begin;
+    const bool has_tail = p.K % BK != 0 && s_begin + nk == slices;
 
-    // ---- loader: A (and W, k-contiguous) as 128-byte LDS rows of 64 k, chunk c of row r in slot c ^ swz(r)
+    // ---- loader: A (and W, k-contiguous) as 128-byte LDS rows of 64 k, chunk c of row r in slot c ^ swz(r); W, transposed: LDS
+    // rows of TBN columns, 16-byte chunk u of row r in slot u ^ 4 (r % 4)
     const uint32_t lda = (uint32_t)p.K * 2u, ldw = p.pitch ? (uint32_t)BK * 2u : (uint32_t)p.ldw * 2u;
-    uint32_t offA[TM], offB[TN];
-    const int last_m = (int)(p.M - m0 < TBM ? p.M - m0 : TBM), last_n = (int)(p.N - n0 < TBN ? p.N - n0 : TBN);
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int r = 8 * (TM * wave + i) + (lane >> 3);
-        offA[i] = r < last_m ? (uint32_t)r * lda + (uint32_t)(((lane & 7) ^ swz(r)) << 4) : OUT_OF_RANGE;
-    }
-    // W, transposed: LDS rows of TBN columns, 16-byte chunk u of row r in slot u ^ 4 (r % 4)
     constexpr int SLOTS = TBN / 8, RPL = 64 / SLOTS;      // chunks of a row, rows of a load
-#pragma unroll
-    for (int i = 0; i < TN; ++i) {
-        if (TRANSPOSED) {
-            const int r = (TN * wave + i) * RPL + lane / SLOTS, u = (lane % SLOTS) ^ ((r & 3) << 2);
-            offB[i] = 8 * u < last_n ? (uint32_t)r * ldw + (p.pitch ? (uint32_t)(u >> 3) * (BM * BK * 2) + (uint32_t)(u & 7) * 16u : (uint32_t)u * 16u)
-                                     : OUT_OF_RANGE;
-        } else {
-            const int r = 8 * (TN * wave + i) + (lane >> 3), w = r % (16 * TN);
-            const int n = r - w + column_of(w >> 4, w & 15);
-            offB[i] = n < last_n ? (uint32_t)n * ldw + (uint32_t)(((lane & 7) ^ swz(r)) << 4) : OUT_OF_RANGE;
-        }
-    }
+    uint32_t offA[TM], offB[TN];
+    uint64_t gA = 0, gB = 0;
+    int64_t load_n0 = 0;
+    int iss_k = 0, iss_tile = 0;
+    uint32_t iss_to = lds_base + (uint32_t)(TM * wave) * 1024u;      // (a stage is as large as a power of two, the LDS begins at 0)
     auto w_address = [&](int64_t k0) {      // W's tile at slice k0
         if (TRANSPOSED)
-            return reinterpret_cast<uint64_t>(p.W) + (p.pitch ? (uint64_t)(((k0 / BM) * (p.pitch / BK) + n0 / BK) * (BM * BK) + (k0 % BM) * BK) * 2u
-                                                              : (uint64_t)(k0 * p.ldw + n0) * 2u);
-        return reinterpret_cast<uint64_t>(p.W) + (p.pitch ? (uint64_t)(((n0 / BM) * (p.pitch / BK) + k0 / BK) * (BM * BK) + (n0 % BM) * BK) * 2u
-                                                          : (uint64_t)(n0 * p.ldw + k0) * 2u);
+            return reinterpret_cast<uint64_t>(p.W) + (p.pitch ? (uint64_t)(((k0 / BM) * (p.pitch / BK) + load_n0 / BK) * (BM * BK) + (k0 % BM) * BK) * 2u
+                                                              : (uint64_t)(k0 * p.ldw + load_n0) * 2u);
+        return reinterpret_cast<uint64_t>(p.W) + (p.pitch ? (uint64_t)(((load_n0 / BM) * (p.pitch / BK) + k0 / BK) * (BM * BK) + (load_n0 % BM) * BK) * 2u
+                                                          : (uint64_t)(load_n0 * p.ldw + k0) * 2u);
     };
-    auto issue = [&](int s) {
-        const int64_t k0 = (s_begin + s) * BK;
-        const u32x4 ra = descriptor(reinterpret_cast<uint64_t>(p.A) + (uint64_t)(m0 * p.K + k0) * 2u);
-        const u32x4 rb = descriptor(w_address(k0));
-        const uint32_t dst = lds_base + (uint32_t)(s & 1) * STAGE_BYTES;
-        const int left = (int)(p.K - k0 < BK ? p.K - k0 : BK);      // (a multiple of eight)
+    const int k_left = (int)(p.K - (int64_t)(slices - 1) * BK);      // of the last slice (a multiple of eight)
+    auto cut_tail = [&]() {                                          // the loads to come are those of the last slice
+        const int lane = here(threadIdx.x & 63), wave = here_scalar(wave0);
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const int r = 8 * (TM * wave + i) + (lane >> 3);
-            buffer_to_lds_16(dst + (uint32_t)(TM * wave + i) * 1024u, ra, 8 * ((lane & 7) ^ swz(r)) < left ? offA[i] : OUT_OF_RANGE);
+            if (8 * ((lane & 7) ^ swz(r)) >= k_left) offA[i] = OUT_OF_RANGE;
         }
 #pragma unroll
         for (int i = 0; i < TN; ++i) {
-            bool in;
+            const int r = TRANSPOSED ? (TN * wave + i) * RPL + lane / SLOTS : 8 * (TN * wave + i) + (lane >> 3);
+            if ((TRANSPOSED ? r : 8 * ((lane & 7) ^ swz(r))) >= k_left) offB[i] = OUT_OF_RANGE;
+        }
+    };
+    auto enter_tile = [&](int ordinal) {
+        const int lane = here(threadIdx.x & 63), wave = here_scalar(wave0);
+        int64_t m0;
+        tile_origin(ordinal, m0, load_n0);
+        const int last_m = (int)(p.M - m0 < TBM ? p.M - m0 : TBM), last_n = (int)(p.N - load_n0 < TBN ? p.N - load_n0 : TBN);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int r = 8 * (TM * wave + i) + (lane >> 3);
+            offA[i] = r < last_m ? (uint32_t)r * lda + (uint32_t)(((lane & 7) ^ swz(r)) << 4) : OUT_OF_RANGE;
+        }
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
             if (TRANSPOSED) {
-                in = (TN * wave + i) * RPL + lane / SLOTS < left;
+                const int r = (TN * wave + i) * RPL + lane / SLOTS, u = (lane % SLOTS) ^ ((r & 3) << 2);
+                offB[i] = 8 * u < last_n ? (uint32_t)r * ldw + (p.pitch ? (uint32_t)(u >> 3) * (BM * BK * 2) + (uint32_t)(u & 7) * 16u : (uint32_t)u * 16u)
+                                         : OUT_OF_RANGE;
             } else {
-                const int r = 8 * (TN * wave + i) + (lane >> 3);
-                in = 8 * ((lane & 7) ^ swz(r)) < left;
+                const int r = 8 * (TN * wave + i) + (lane >> 3), w = r % (16 * TN);
+                const int n = r - w + column_of(w >> 4, w & 15);
+                offB[i] = n < last_n ? (uint32_t)n * ldw + (uint32_t)(((lane & 7) ^ swz(r)) << 4) : OUT_OF_RANGE;
             }
-            buffer_to_lds_16(dst + A_BYTES + (uint32_t)(TN * wave + i) * 1024u, rb, in ? offB[i] : OUT_OF_RANGE);
+        }
+        gA = uniform64(reinterpret_cast<uint64_t>(p.A) + (uint64_t)(m0 * p.K + (int64_t)s_begin * BK) * 2u);
+        gB = uniform64(w_address((int64_t)s_begin * BK));
+        if (has_tail && nk == 1) cut_tail();
+    };
+    auto issue_one = [&](auto J) {
+        constexpr int j = decltype(J)::value;
+        static_assert(TM == TN, "one base of both operands' loads");
+        if constexpr (j < TM)
+            buffer_to_lds_16<j * 1024u>(iss_to, descriptor(gA), offA[j]);
+        else
+            buffer_to_lds_16<A_BYTES + (j - TM) * 1024u>(iss_to, descriptor(gB), offB[j - TM]);
+    };
+    // from a slice of W to the next; blocks of 256 rows, transposed: every fourth slice begins another block
+    const uint64_t stepB = TRANSPOSED ? (p.pitch ? BK * BK * 2 : (uint64_t)p.ldw * (BK * 2)) : p.pitch ? BM * BK * 2 : BK * 2;
+    const uint64_t jumpB = TRANSPOSED && p.pitch ? (uint64_t)(p.pitch / BK - 1) * (BM * BK * 2) : 0;
+    auto issue_done = [&]() {      // the load cursor moves on by a slice
+        iss_to ^= STAGE_BYTES;
+        iss_k = __builtin_amdgcn_readfirstlane(iss_k + 1);
+        if (iss_k < nk) {
+            gA += BK * 2;
+            gB += stepB;
+            if (TRANSPOSED && ((s_begin + iss_k) & (BM / BK - 1)) == 0) gB += jumpB;
+            if (has_tail && iss_k + 1 == nk) cut_tail();
+        } else {
+            iss_k = 0;
+            ++iss_tile;
+            enter_tile(iss_tile < n_my ? iss_tile : n_my - 1);      // (past the last tile: loads that are never read)
+        }
+    };
+
+    // ---- fragments: lane (q, c) supplies row c of 16 and k = 8 q .. 8 q + 7 of the 32 of a k-step
+    uint32_t ra[4], rb[4], rf[4];
+    auto transposed_at = [&](int q, int row) {      // byte of the lane's piece of MFMA tiles 2 q, 2 q + 1 (8 bytes further), LDS row `row`
+        return (uint32_t)row * (TBN * 2) + (uint32_t)((((wn0 >> 3) + 4 * q) ^ ((l16 >> 2) << 2)) + (l16 & 3)) * 16u;
+    };
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const int r = wm0 + 16 * (t % TM) + l16, rn = wn0 + 16 * (t % TN) + l16;
+        ra[t] = (uint32_t)(r * 128 + ((quad ^ swz(r)) << 4));
+        rb[t] = A_BYTES + (TRANSPOSED ? transposed_at(t, 8 * quad + (l16 >> 2)) : (uint32_t)(rn * 128 + ((quad ^ swz(rn)) << 4)));
+        rf[t] = F_OFF + transposed_at(t, 8 * (quad & 1) + (l16 >> 2));
+    }
+    struct Frags {
+        bf16x8 a[TM];
+        s16x4 b[TN][2];
+    };
+    // The i-th fragment read of a k-step: W's first, the rows' all, W's others.
+    auto read_one = [&](Frags& f, int ks, int i) {
+        constexpr int PER = TRANSPOSED ? 2 : 1;
+        if (i >= PER && i < PER + TM) {
+            const int t = i - PER;
+            f.a[t] = *reinterpret_cast<const bf16x8*>(lds + (ra[t & 3] ^ (64u * ks)) + (t >> 2) * 64 * 128);
+            return;
+        }
+        const int j = i < PER ? i : i - TM, t = j / PER;
+        if (TRANSPOSED) {
+            f.b[t][j % 2] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_s16x4*)(lds + rb[t >> 1] + (t & 1) * 8 + ks * 32 * (TBN * 2) + (j % 2) * 4 * (TBN * 2)));
+        } else {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(lds + (rb[t & 3] ^ (64u * ks)) + (t >> 2) * 64 * 128);
+            f.b[t][0] = __builtin_bit_cast(s16x4, u32x2{v[0], v[1]});
+            f.b[t][1] = __builtin_bit_cast(s16x4, u32x2{v[2], v[3]});
+        }
+    };
+    auto b_of = [](const Frags& f, int t) {
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(f.b[t][0], f.b[t][1], 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto flip_stage = [&]() {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            ra[t] ^= STAGE_BYTES;
+            rb[t] ^= STAGE_BYTES;
         }
     };
 
     floatx4 acc[TM][TN];
+    int mine[TM];                     // block of the lane's row of each MFMA tile
+
+    // ---- the blocks' part of a tile; whether a factor is not finite
+    auto blocks_part = [&](int64_t m0, int64_t n0) {
+        bool special = false;         // whether the wavefront has met a factor that is not finite
+        const int lane = here(threadIdx.x & 63), l16 = lane & 15, quad = lane >> 4, wave = here_scalar(wave0);
+        uint64_t left[TBM / 64];      // rows of the tile whose block is still to come
+        int block[TBM / 64];
 #pragma unroll
-    for (int ta = 0; ta < TM; ++ta)
+        for (int i = 0; i < TBM / 64; ++i) {
+            const int64_t m = m0 + 64 * i + lane;
+            block[i] = m < p.M ? p.row_adapter[m] : ROW_OUTSIDE;
+            left[i] = __builtin_amdgcn_ballot_w64(block[i] >= 0);
+        }
+        const int pitch = adapter_pitch(p.rank);
+        const uint16_t* const hx = p.Hx + (m0 + wm0 + l16) * (2 * pitch) + 8 * quad;
+        for (;;) {
+            int a = -1;
 #pragma unroll
-        for (int tb = 0; tb < TN; ++tb) acc[ta][tb] = floatx4{0.f, 0.f, 0.f, 0.f};
-    if (nk > 0) issue(0);
-    if (nk > 1) issue(1);
-    for (int s = 0; s < nk; ++s) {
-        if (s + 1 < nk)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(TM + TN) : "memory");
-        else
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        const char* const stage = lds + (uint32_t)(s & 1) * STAGE_BYTES;
+            for (int i = 0; i < TBM / 64; ++i)
+                if (a < 0 && left[i]) a = __builtin_amdgcn_readlane(block[i], (int)__builtin_ctzll(left[i]));
+            if (a < 0) break;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            bf16x8 a[TM], b[TN];
+            for (int i = 0; i < TBM / 64; ++i) left[i] &= ~__builtin_amdgcn_ballot_w64(block[i] == a);
+            int rank = p.ranks ? p.ranks[a] : p.rank;
+            rank = __builtin_amdgcn_readfirstlane(rank < p.rank ? rank : p.rank);
+            const uint64_t factors = uniform64(reinterpret_cast<uint64_t>(p.F) + (uint64_t)((int64_t)a * p.rank * p.N + n0) * 2u);
+            for (int r0 = 0; r0 < rank; r0 += 64) {
+                // up to four chunks of 16 pairs: LDS rows of TBN columns as W's, transposed
+                constexpr int F_LOADS = (int)(4 * F_CHUNK / 1024 / 4);      // of a wavefront
+                __syncthreads();                   // (the chunks before have been read)
 #pragma unroll
-            for (int t = 0; t < TM; ++t) {
-                const int r = wm0 + 16 * t + l16;
-                a[t] = *reinterpret_cast<const bf16x8*>(stage + r * 128 + (((4 * ks + quad) ^ swz(r)) << 4));
-            }
+                for (int i = 0; i < F_LOADS; ++i) {
+                    const int idx = 4 * i + wave, r = idx * RPL + lane / SLOTS, u = (lane % SLOTS) ^ ((r & 3) << 2);
+                    const bool in = r0 + r < rank && n0 + 8 * u < p.N;
+                    if (r0 + 16 * (idx * RPL / 16) < rank)
+                        buffer_to_lds_16<F_OFF>(lds_base + (uint32_t)idx * 1024u, descriptor(factors),
+                                         in ? (uint32_t)(r0 + r) * (uint32_t)(p.N * 2) + (uint32_t)u * 16u : OUT_OF_RANGE);
+                }
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+                for (int c = 0; 16 * c < 64 && r0 + 16 * c < rank; ++c) {
+                    u32x4 f[TN];
+                    uint32_t least = 0x7f807f80u;      // of both halves; 0: not finite
 #pragma unroll
-            for (int t = 0; t < TN; ++t) {
-                if (TRANSPOSED) {
-                    // lane i of a group: row i / 4 of four, columns of piece i % 4 (column_of(t, 4 (i % 4)) ..)
-                    const int r = 32 * ks + 8 * quad + (l16 >> 2), n = wn0 + column_of(t, 4 * (l16 & 3));
-                    const uint32_t at = A_BYTES + (uint32_t)r * (TBN * 2) + (uint32_t)(((n >> 3) ^ ((r & 3) << 2)) << 4) + (uint32_t)(n & 7) * 2u;
-                    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(stage + at));
-                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(stage + at + 4 * (TBN * 2)));
-                    b[t] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-                } else {
-                    const int r = wn0 + 16 * t + l16;
-                    b[t] = *reinterpret_cast<const bf16x8*>(stage + A_BYTES + r * 128 + (((4 * ks + quad) ^ swz(r)) << 4));
+                    for (int t = 0; t < TN; ++t) {
+                        const char* const at = lds + rf[t >> 1] + c * F_CHUNK + (t & 1) * 8;
+                        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+                        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * (TBN * 2)));
+                        f[t] = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    }
+#pragma unroll
+                    for (int t = 0; t < TN; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t w = f[t][e];
+                            least = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, least),
+                                                                                           __builtin_bit_cast(u16x2, ~w & 0x7f807f80u)));
+                        }
+                    if (__builtin_amdgcn_ballot_w64((least & 0xffffu) == 0 || least >> 16 == 0)) {
+                        special = true;
+#pragma unroll
+                        for (int t = 0; t < TN; ++t)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                uint32_t w = f[t][e];
+                                if ((~w & 0x7f80u) == 0) w &= 0xffff0000u;
+                                if ((~w & 0x7f800000u) == 0) w &= 0xffffu;
+                                f[t][e] = w;
+                            }
+                    }
+#pragma unroll
+                    for (int ta = 0; ta < TM; ++ta) {
+                        const bool use = mine[ta] == a;
+                        if (__builtin_amdgcn_ballot_w64(use) == 0) continue;
+                        u32x4 h = {0u, 0u, 0u, 0u};
+                        if (use) h = *reinterpret_cast<const u32x4*>(hx + (int64_t)(16 * ta) * (2 * pitch) + 2 * (r0 + 16 * c));
+#pragma unroll
+                        for (int tb = 0; tb < TN; ++tb)
+                            acc[ta][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f[tb]), __builtin_bit_cast(bf16x8, h), acc[ta][tb], 0, 0, 0);
+                    }
                 }
             }
-#pragma unroll
-            for (int tb = 0; tb < TN; ++tb)
-#pragma unroll
-                for (int ta = 0; ta < TM; ++ta) acc[ta][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[tb], a[ta], acc[ta][tb], 0, 0, 0);
         }
-        if (s + 2 < nk) {
-            __syncthreads();                 // every wavefront has read the stage
-            issue(s + 2);
+        return special;
+    };
+    // The products with factors that are not finite, which none of the stored sums has: an infinity or a not-a-number each, so
+    // the sum's rounding does not matter.  The lanes go through their own pieces of the tile once more.
+    auto add_special = [&](int64_t m0, int64_t n0) {
+        const int pitch = adapter_pitch(p.rank), lane = here(threadIdx.x & 63), l16 = lane & 15, quad = lane >> 4;
+#pragma unroll 1
+        for (int k = 0; k < TM * TN / 2; ++k) {
+            const int64_t m = m0 + wm0 + 16 * (k / (TN / 2)) + l16, n = n0 + wn0 + 32 * (k % (TN / 2)) + 8 * quad;
+            const int a = m < p.M && n < p.N ? p.row_adapter[m] : ROW_OUTSIDE;
+            if (a < 0) continue;
+            int rank = p.ranks ? p.ranks[a] : p.rank;
+            rank = rank < p.rank ? rank : p.rank;
+            uint16_t* const out = p.out + m * p.N + n;
+#pragma unroll 1
+            for (int r = 0; r < rank; ++r) {
+                const float h = p.H[m * pitch + r];
+#pragma unroll 1
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t bits = (uint32_t)p.F[((int64_t)a * p.rank + r) * p.N + n + e] << 16;
+                    if ((~bits & 0x7f800000u) == 0)
+                        out[e] = (uint16_t)pack_bf16(fmaf(h, __uint_as_float(bits), __uint_as_float((uint32_t)out[e] << 16)), 0.f);
+                }
+            }
         }
+    };
+
+    auto epilogue = [&](int64_t m0, int64_t n0) {
+        // register i of lane (q, c) of tile (ta, tb): row 16 ta + c, column column_of(tb, 4 q + i)
+        mfma_settle();
+        const int lane = here(threadIdx.x & 63), l16 = lane & 15, quad = lane >> 4;
+#pragma unroll
+        for (int ta = 0; ta < TM; ++ta) {
+            const int64_t m = m0 + wm0 + 16 * ta + l16;
+            if (SPLIT) {
+                if (m >= p.M) continue;
+                float* const row = p.planes + ((int64_t)blockIdx.y * p.M + m) * p.N + n0 + wn0;
+#pragma unroll
+                for (int tb = 0; tb < TN; ++tb) {
+                    const int n = column_of(tb, 4 * quad);
+                    float x[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = acc_read(acc[ta][tb][e]);
+                    if (n0 + wn0 + n < p.N) *reinterpret_cast<floatx4*>(row + n) = floatx4{x[0], x[1], x[2], x[3]};
+                }
+            } else {
+                if (mine[ta] == ROW_OUTSIDE) continue;
+                uint16_t* const row = p.out + m * p.N + n0 + wn0;
+#pragma unroll
+                for (int tb = 0; tb < TN; tb += 2) {
+                    const int n = column_of(tb, 4 * quad);
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = acc_read(acc[ta][tb + (e >> 2)][e & 3]);
+                    if (n0 + wn0 + n >= p.N) continue;
+                    *reinterpret_cast<u32x4*>(row + n) = u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+                }
+            }
+        }
+    };
+
+    // ---- pipeline: slice s lives in stage s & 1; f0 holds the fragments of its first k-step, f1 of the second
+    Frags f0, f1;
+    enter_tile(0);
+#pragma unroll 1
+    for (int s = 0; s < 2; ++s) {
+        static_for<0, LOADS>(issue_one);
+        issue_done();
     }
-    // register i of lane (q, c) of tile (ta, tb): row 16 ta + c, column column_of(tb, 4 q + i)
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+    __syncthreads();
 #pragma unroll
-    for (int ta = 0; ta < TM; ++ta) {
-        const int64_t m = m0 + wm0 + 16 * ta + l16;
-        if (m >= p.M) continue;
-        float* const row = p.planes + ((int64_t)blockIdx.y * p.M + m) * p.N + n0 + wn0;
+    for (int i = 0; i < READS; ++i) read_one(f0, 0, i);
+
+    auto slice_body = [&]() {
+        auto mfma = [&](const Frags& f, auto J) {
+            constexpr int j = decltype(J)::value, tb = j / TM, ta = j % TM;
+            acc[ta][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b_of(f, tb), f.a[ta], acc[ta][tb], 0, 0, 0);
+        };
+        // k-step 0 on f0; the reads of k-step 1 go out over its first three quarters
+        static_for<0, STEP>([&](auto J) {
+            constexpr int j = decltype(J)::value, M34 = 3 * STEP / 4;
+            mfma(f0, J);
+            if constexpr (j < M34)
+                static_for<first_slot(j, READS, M34), first_slot(j + 1, READS, M34)>([&](auto I) { read_one(f1, 1, decltype(I)::value); });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        __syncthreads();                                   // every wavefront has read the stage
+        // the first half of k-step 1 on f1; the first loads of slice s + 2
+        static_for<0, BPOS>([&](auto J) {
+            constexpr int j = decltype(J)::value;
+            mfma(f1, J);
+            static_for<first_slot(j, N2B, BPOS), first_slot(j + 1, N2B, BPOS)>([&](auto I) { issue_one(I); });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N2B) : "memory");      // everything but those: slice s + 1 is in LDS
+        __syncthreads();
+        flip_stage();
+        // the rest of k-step 1; the reads of the next slice's k-step 0, the other loads
+        static_for<BPOS, STEP>([&](auto J) {
+            constexpr int j = decltype(J)::value - BPOS, M = STEP - BPOS;
+            mfma(f1, J);
+            static_for<first_slot(j, READS, M - STEP / 8), first_slot(j + 1, READS, M - STEP / 8)>([&](auto I) { read_one(f0, 0, decltype(I)::value); });
+            static_for<first_slot(j, N3, M), first_slot(j + 1, N3, M)>([&](auto I) { issue_one(std::integral_constant<int, N2B + decltype(I)::value>{}); });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        issue_done();
+    };
+    for (int t = 0; t < n_my; ++t) {
+        int64_t m0, n0;
+        tile_origin(t, m0, n0);
+        bool special = false;
 #pragma unroll
-        for (int tb = 0; tb < TN; ++tb) {
-            const int n = column_of(tb, 4 * quad);
-            if (n0 + wn0 + n < p.N) *reinterpret_cast<floatx4*>(row + n) = acc[ta][tb];
+        for (int ta = 0; ta < TM; ++ta)
+#pragma unroll
+            for (int tb = 0; tb < TN; ++tb) acc[ta][tb] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (!SPLIT) {
+#pragma unroll
+            for (int ta = 0; ta < TM; ++ta) {
+                const int64_t m = m0 + wm0 + 16 * ta + l16;
+                mine[ta] = m < p.M ? p.row_adapter[m] : ROW_OUTSIDE;
+            }
+            special = blocks_part(m0, n0);
         }
+        for (int k = 0; k < nk; ++k) slice_body();
+        epilogue(m0, n0);
+        if (!SPLIT && special) add_special(m0, n0);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no load may be in flight when the workgroup's LDS is released
 }
 
-template <int TM, int TN>
-hipError_t launch_base(BaseParams& p, bool transposed, DeviceInfo& dev, hipStream_t stream)
+template <int TM, int TN, bool TRANSPOSED, bool SPLIT>
+hipError_t launch_base(BaseParams& p, DeviceInfo& dev, hipStream_t stream)
 {
-    constexpr int lds = 2 * (TM + TN) * 32 * 128;
+    constexpr int stages = 2 * (TM + TN) * 32 * 128, lds = stages + 4 * 16 * TN * 32 * 2;
+    constexpr int slot = (TM == 8 ? 4 : 0) + (TRANSPOSED ? 2 : 0) + (SPLIT ? 1 : 0);
+    if (!dev.adapter_base_lds_set[slot]) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&adapter_base_kernel<TM, TN, TRANSPOSED, SPLIT>),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+        dev.adapter_base_lds_set[slot] = true;
+    }
     p.tiles_m = (int)((p.M + 32 * TM - 1) / (32 * TM));
     p.tiles_n = (int)((p.N + 32 * TN - 1) / (32 * TN));
     p.group_m = 8;
-    const dim3 grid((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.split);
-    if (transposed)
-        adapter_base_kernel<TM, TN, true><<<grid, 256, lds, stream>>>(p);
-    else
-        adapter_base_kernel<TM, TN, false><<<grid, 256, lds, stream>>>(p);
+    const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n, slots = (int64_t)(dev.cus > 0 ? dev.cus : 256) * (TM == 8 ? 1 : 2);
+    const dim3 grid((unsigned)(tiles < slots || SPLIT ? tiles : slots), (unsigned)p.split);
+    adapter_base_kernel<TM, TN, TRANSPOSED, SPLIT><<<grid, 256, lds, stream>>>(p);
     return hipGetLastError();
 }
 
 }  // namespace
 
-int adapter_base_split(int64_t, int64_t, int64_t) { return 1; }
+// Ways the contraction is divided along k: fewer tiles than half of what the chip holds at once, and at least four slices each.
+int adapter_base_split(int64_t M, int64_t N, int64_t K)
+{
+    const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128), slices = (K + BK - 1) / BK;
+    if (tiles <= 0 || tiles >= 256) return 1;
+    const int64_t s = 512 / tiles < slices / 4 ? 512 / tiles : slices / 4;
+    return s < 2 ? 1 : s > 16 ? 16 : (int)s;
+}
 
 hipError_t launch_adapter_base_bf16(const AdapterBase& a, DeviceInfo& dev, hipStream_t stream)
 {
@@ -219,8 +523,18 @@ hipError_t launch_adapter_base_bf16(const AdapterBase& a, DeviceInfo& dev, hipSt
     p.pitch = a.blocked ? bf16_pitch(p.ldw) : 0;
     p.planes = a.planes;
     p.split = a.split;
+    p.out = a.out;
+    p.row_adapter = a.row_adapter;
+    p.Hx = a.Hx;
+    p.H = a.H;
+    p.F = a.F;
+    p.ranks = a.ranks;
+    p.rank = a.rank;
     p.num_xcd = dev.xcds > 0 ? dev.xcds : 1;
-    return launch_base<4, 4>(p, a.transposed, dev, stream);
+    const int64_t big = ((a.M + 255) / 256) * ((a.N + 255) / 256);
+    if (a.split > 1) return a.transposed ? launch_base<4, 4, true, true>(p, dev, stream) : launch_base<4, 4, false, true>(p, dev, stream);
+    if (big >= 256) return a.transposed ? launch_base<8, 8, true, false>(p, dev, stream) : launch_base<8, 8, false, false>(p, dev, stream);
+    return a.transposed ? launch_base<4, 4, true, false>(p, dev, stream) : launch_base<4, 4, false, false>(p, dev, stream);
 }
 
 }  // namespace sfb

@@ -1031,8 +1031,8 @@ static int check_adapters(int64_t J, int64_t D, int64_t T, const sfb_adapters* a
 // The workspace of either call: the block of each row, the projections (forward H; backward H and dH), the product with the
 // shared matrix (N columns, contracted over K) and what its contraction needs itself.
 struct AdapterLayout {
-    int64_t off_h, off_dh, off_planes, off_partial, total;
-    int split;
+    int64_t off_h, off_dh, off_terms, off_planes, off_partial, total;
+    int split;      // 1 with bf16 blocks: one kernel makes the whole output
 };
 static AdapterLayout adapter_layout(int64_t T, int64_t N, int64_t K, const sfb_adapters* ad, bool backward)
 {
@@ -1040,10 +1040,12 @@ static AdapterLayout adapter_layout(int64_t T, int64_t N, int64_t K, const sfb_a
     const int64_t h = round_up(T * sfb::adapter_pitch(ad->rank) * 4);
     l.off_h = round_up(T * 4);
     l.off_dh = l.off_h + h;
-    l.off_planes = l.off_dh + (backward ? h : 0);
-    l.split = ad->dtype == SFB_BF16 ? sfb::adapter_base_split(T, N, K) : 1;
-    l.off_partial = l.off_planes + round_up(l.split * T * N * 4);
-    l.total = l.off_partial + (ad->dtype == SFB_F32 && T > 0 ? round_up(sfb::gemm_f32_partial_bytes(T, N, K)) : 0);
+    l.off_terms = l.off_dh + (backward ? h : 0);
+    const bool bf16 = ad->dtype == SFB_BF16;
+    l.split = bf16 ? sfb::adapter_base_split(T, N, K) : 1;
+    l.off_planes = l.off_terms + (bf16 ? h : 0);
+    l.off_partial = l.off_planes + (bf16 && l.split == 1 ? 0 : round_up(l.split * T * N * 4));
+    l.total = l.off_partial + (!bf16 && T > 0 ? round_up(sfb::gemm_f32_partial_bytes(T, N, K)) : 0);
     return l;
 }
 
@@ -1103,7 +1105,15 @@ static int adapter_output(sfb_ctx* ctx, const AdapterLayout& l, const void* src,
         b.M = T; b.N = N; b.K = K;
         b.planes = planes;
         b.split = l.split;
+        b.out = static_cast<uint16_t*>(out);
+        b.row_adapter = reinterpret_cast<const int32_t*>(ctx->ws);
+        b.Hx = reinterpret_cast<const uint16_t*>(ctx->ws + l.off_terms);
+        b.H = H;
+        b.F = static_cast<const uint16_t*>(factors);
+        b.ranks = ad->ranks;
+        b.rank = ad->rank;
         SFB_RUN(KID_ADAPTER_BASE, sfb::launch_adapter_base_bf16(b, ctx->dev, ctx->stream));
+        if (l.split == 1) return SFB_OK;
     } else {
         int parts = 1;
         sfb::GemmF32Args g = {};
@@ -1170,6 +1180,7 @@ int sfb_adapter_forward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J,
     a.K = D;
     a.H = reinterpret_cast<float*>(ctx->ws + l.off_h);
     a.H_out = H;
+    if (a.bf16 && l.split == 1) a.Hx = reinterpret_cast<uint16_t*>(ctx->ws + l.off_terms);
     SFB_RUN(KID_ADAPTER_PROJECT, sfb::launch_adapter_project(a, ctx->dev, ctx->stream));
     return adapter_output(ctx, l, X, W, Wb, blocked, false, T, J, D, ad, ad->U, a.H, Y);
 }
@@ -1205,6 +1216,7 @@ int sfb_adapter_backward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J
     a.F = ad->U;
     a.K = J;
     a.H = dH;
+    if (a.bf16 && l.split == 1) a.Hx = reinterpret_cast<uint16_t*>(ctx->ws + l.off_terms);
     SFB_RUN(KID_ADAPTER_PROJECT, sfb::launch_adapter_project(a, ctx->dev, ctx->stream));
     if (dX && rows) {
         rc = adapter_output(ctx, l, dY, W, Wb, blocked, true, T, D, J, ad, ad->V, dH, dX);
