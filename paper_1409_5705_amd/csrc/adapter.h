@@ -23,7 +23,8 @@ __host__ __device__ inline int adapter_pitch(int rank) { return (rank + 15) / 16
 constexpr int ROW_NONE = -1, ROW_OUTSIDE = -2;      // row_adapter: a request without a block; no request at all
 
 // H[t][r] = scale_a sum_k X[t][k] F_a[r][k], F [count][rank][K] of X's type; zeros for r >= ranks[a] and for rows without a
-// block.  row_adapter[t] (written): the block of row t, ROW_NONE or ROW_OUTSIDE.  H: [T][adapter_pitch(rank)] fp32;
+// block.  row_adapter[t] (written): the block of row t, ROW_NONE or ROW_OUTSIDE (a `start` that is not as it has to be may
+// leave entries as they were: what reads them passes over numbers outside the pool).  H: [T][adapter_pitch(rank)] fp32;
 // H_out (nullable): [T][rank], rows of a request only.
 struct AdapterProjectArgs {
     AdapterRows rows;
@@ -55,6 +56,7 @@ struct AdapterBase {
     const float* H;
     const uint16_t* F;
     const int32_t* ranks;
+    int64_t count;
     int rank;
 };
 hipError_t launch_adapter_base_bf16(const AdapterBase& a, DeviceInfo& dev, hipStream_t stream);
@@ -68,6 +70,7 @@ struct AdapterJoinArgs {
     const float* H;            // [T][adapter_pitch(rank)]
     const void* F;
     const int32_t* ranks;
+    int64_t count;
     int rank;
     void* out;
     bool bf16;

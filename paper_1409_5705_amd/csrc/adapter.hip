@@ -17,20 +17,22 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float bf16_float(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 
-// The request of row t, or -1 (empty requests are passed over: the last q with start[q] <= t).
-__device__ __forceinline__ int64_t request_of(const int64_t* start, int64_t requests, int64_t t)
+// The request of row t, or -1 (empty requests are passed over: the last q with start[q] <= t).  By a whole wavefront: 64
+// probes a step.
+__device__ __forceinline__ int64_t request_of(const int64_t* start, int64_t requests, int64_t t, int lane)
 {
     if (requests <= 0 || t < start[0] || t >= start[requests]) return -1;
-    int64_t lo = 0, hi = requests;
-    while (hi - lo > 1) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (start[mid] <= t)
-            lo = mid;
-        else
-            hi = mid;
+    int64_t lo = 0, n = requests;                  // start[lo] <= t; the answer is in [lo, lo + n)
+    while (n > 1) {
+        const int64_t step = (n + 63) / 64, at = lane * step;
+        const uint64_t below = __builtin_amdgcn_ballot_w64(at < n && start[lo + at] <= t);
+        const int64_t k = 63 - __builtin_clzll(below | 1);
+        lo += k * step;
+        n = n - k * step < step ? n - k * step : step;
     }
     return lo;
 }
@@ -40,16 +42,20 @@ __device__ __forceinline__ int rank_of(const int32_t* ranks, int rank, int64_t a
     return r < 0 ? 0 : r < rank ? r : rank;
 }
 
-// 16 bytes of a row (eight bf16, four fp32) from element k on; what lies at or behind `end` is zero.  VEC: rows are 16-byte
-// aligned and `end` is a multiple of the elements.
-template <typename T, bool VEC>
+// 16 bytes of a row (eight bf16, four fp32).  fp32 rows need not be 16-byte aligned.
+typedef u32x4 u32x4_by_word __attribute__((aligned(4)));
+template <typename T>
+__device__ __forceinline__ u32x4 load_chunk(const T* p)
+{
+    return *reinterpret_cast<const u32x4_by_word*>(p);
+}
+// The same from element k of a row on; what lies at or behind `end` is zero (bf16: a multiple of eight).
+template <typename T>
 __device__ __forceinline__ u32x4 load_chunk(const T* row, int64_t k, int64_t end)
 {
     u32x4 v = {0u, 0u, 0u, 0u};
-    if (VEC) {
-        if (k < end) v = *reinterpret_cast<const u32x4*>(row + k);
-    } else {
-        static_assert(VEC || sizeof(T) == 4, "bf16 rows are 16-byte aligned");
+    if (k + 16 / (int)sizeof(T) <= end) return load_chunk(row + k);
+    if (sizeof(T) == 4) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (k + e < end) v[e] = *reinterpret_cast<const uint32_t*>(row + k + e);
@@ -96,114 +102,121 @@ __device__ __forceinline__ void two_terms(float v, uint16_t& first, uint16_t& se
 __device__ __forceinline__ int term_at(int r) { return (r >> 4) * 32 + (r & 15); }
 
 constexpr int64_t MAX_BLOCKS = 1 << 22;      // workgroups of a launch (threads of a grid are counted in 32 bits)
-constexpr int PW = 8;      // wavefronts that share k
+constexpr int PW = 16;      // wavefronts that share k
 
-// Rows ROWS * blockIdx.x .. of X against the 16 RT factors 16 RT * blockIdx.y ..; the eight wavefronts share k.
-template <typename T, bool VEC, int RT, int ROWS>
-__global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams p)
+// Up to 16 rows of one request against the 16 RT factors 16 RT * blockIdx.y ..; the wavefronts share k.  Workgroup w < windows
+// takes the rows from 16 w on, workgroup windows + q those from the first row of request q on, both to the next multiple of 16
+// or to the end of their request: every row once, and never two blocks in a workgroup.  (Tiles of 32 rows whatever the requests,
+// gone through once for every block in them: 8192 rows in 24 requests, K = 4096, 64 pairs 62 us.)
+// What bounds it is the stream of X: a wavefront's loads of U k-steps are in flight together.
+template <typename T, int RT>
+__global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams p, unsigned windows)
 {
-    constexpr int MT = (ROWS + 15) / 16, CE = 16 / (int)sizeof(T), STEP = 4 * CE;
-    __shared__ int row_of[32];
-    __shared__ floatx4 part[PW][MT * RT][64];
+    constexpr int CE = 16 / (int)sizeof(T), STEP = 4 * CE, U = RT == 1 ? 8 : 4;
+    __shared__ floatx4 part[PW][RT][64];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t t0 = (int64_t)blockIdx.x * ROWS;
     const int r0 = (int)blockIdx.y * 16 * RT;
     const AdapterRows& rows = p.rows;
-    const int n_rows = (int)(rows.T - t0 < ROWS ? rows.T - t0 : ROWS);
-
-    if (tid < 32) {
-        int a = ROW_OUTSIDE;
-        if (tid < n_rows) {
-            const int64_t q = request_of(rows.start, rows.requests, t0 + tid);
-            if (q >= 0) {
-                a = rows.adapter[q];
-                if (a < 0 || a >= rows.count || rank_of(rows.ranks, rows.rank, a) == 0) a = ROW_NONE;
-            }
-            if (blockIdx.y == 0) p.row_adapter[t0 + tid] = a;
-        }
-        row_of[tid] = a;
+    int64_t t0, q;
+    if (blockIdx.x < windows) {
+        t0 = (int64_t)blockIdx.x * 16;
+        const int64_t t = t0 + tid;
+        if (tid < 16 && blockIdx.y == 0 && t < rows.T && (t < rows.start[0] || t >= rows.start[rows.requests])) p.row_adapter[t] = ROW_OUTSIDE;
+        q = request_of(rows.start, rows.requests, t0, lane);
+        if (q < 0) return;
+    } else {
+        q = blockIdx.x - windows;
+        t0 = rows.start[q];
+        if (t0 < 0 || t0 >= rows.T || (t0 & 15) == 0) return;
     }
-    __syncthreads();
-    const int mine = row_of[lane & 31];
-    // rows without a block: zeros
-    for (int i = tid; i < n_rows * 16 * RT; i += 64 * PW) {
-        const int t = i / (16 * RT), r = r0 + i % (16 * RT);
-        if (row_of[t] < 0 && r < p.pitch) {
-            p.H[(t0 + t) * p.pitch + r] = 0.f;
-            if (p.Hx) p.Hx[(t0 + t) * 2 * p.pitch + term_at(r)] = p.Hx[(t0 + t) * 2 * p.pitch + term_at(r) + 16] = 0;
-            if (p.H_out && row_of[t] == ROW_NONE && r < rows.rank) p.H_out[(t0 + t) * rows.rank + r] = 0.f;
+    int64_t t1 = (t0 | 15) + 1;
+    if (rows.start[q + 1] < t1) t1 = rows.start[q + 1];
+    if (rows.T < t1) t1 = rows.T;
+    const int n_rows = (int)(t1 - t0);
+    if (n_rows <= 0) return;
+    int a = rows.adapter[q];
+    const int rank = a < 0 || a >= rows.count ? 0 : rank_of(rows.ranks, rows.rank, a);
+    if (rank == 0) a = ROW_NONE;
+    if (blockIdx.y == 0 && tid < n_rows) p.row_adapter[t0 + tid] = a;
+    if (r0 >= rank) {      // no factors here: zeros
+        for (int i = tid; i < n_rows * 16 * RT; i += 64 * PW) {
+            const int64_t t = t0 + i / (16 * RT);
+            const int r = r0 + i % (16 * RT);
+            if (r < p.pitch) {
+                p.H[t * p.pitch + r] = 0.f;
+                if (p.Hx) p.Hx[t * 2 * p.pitch + term_at(r)] = p.Hx[t * 2 * p.pitch + term_at(r) + 16] = 0;
+            }
+            if (p.H_out && r < rows.rank) p.H_out[t * rows.rank + r] = 0.f;
         }
+        return;
     }
 
     const int64_t steps = (p.K + STEP - 1) / STEP, per = (steps + PW - 1) / PW;
     const int64_t k_begin = wave * per * STEP, k_end = k_begin + per * STEP < p.K ? k_begin + per * STEP : p.K;
-    const T* xr[MT];
+    const T* const x = static_cast<const T*>(p.X) + (t0 + (l16 < n_rows ? l16 : n_rows - 1)) * p.K + CE * quad;
+    const T* f[RT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        const int t = 16 * m + l16;
-        xr[m] = static_cast<const T*>(p.X) + (t0 + (t < n_rows ? t : n_rows - 1)) * p.K;
+    for (int i = 0; i < RT; ++i) {
+        const int r = r0 + 16 * i + l16;
+        f[i] = static_cast<const T*>(p.F) + ((int64_t)a * rows.rank + (r < rank ? r : rank - 1)) * p.K + CE * quad;
     }
-    uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(lane < 32 && mine >= 0);
-    while (left) {
-        const int a = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
-        const uint32_t now = (uint32_t)__builtin_amdgcn_ballot_w64(lane < 32 && mine == a);
-        left &= ~now;
-        const int rank = rank_of(rows.ranks, rows.rank, a);
-        const T* fr[RT];
+    floatx4 acc[RT];
 #pragma unroll
-        for (int f = 0; f < RT; ++f) {
-            const int r = r0 + 16 * f + l16;
-            fr[f] = static_cast<const T*>(p.F) + ((int64_t)a * rows.rank + (r < rank ? r : rank - 1)) * p.K;
-        }
-        floatx4 acc[MT][RT];
+    for (int i = 0; i < RT; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    int64_t k = k_begin;
+    for (; k + U * STEP <= k_end; k += U * STEP) {
+        u32x4 xv[U], fv[U][RT];
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int u = 0; u < U; ++u) {
+            xv[u] = load_chunk(x + k + u * STEP);
 #pragma unroll
-            for (int f = 0; f < RT; ++f) acc[m][f] = floatx4{0.f, 0.f, 0.f, 0.f};
-        for (int64_t k = k_begin; k < k_end; k += STEP) {
-            u32x4 x[MT], w[RT];
-#pragma unroll
-            for (int m = 0; m < MT; ++m) x[m] = load_chunk<T, VEC>(xr[m], k + CE * quad, k_end);
-#pragma unroll
-            for (int f = 0; f < RT; ++f) w[f] = load_chunk<T, VEC>(fr[f], k + CE * quad, k_end);
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int f = 0; f < RT; ++f) acc[m][f] = mfma_chunk<T>(w[f], x[m], acc[m][f]);
+            for (int i = 0; i < RT; ++i) fv[u][i] = load_chunk(f[i] + k + u * STEP);
         }
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int f = 0; f < RT; ++f) part[wave][m * RT + f][lane] = acc[m][f];
-        __syncthreads();
-        const float s = rows.scale ? rows.scale[a] : 1.f;
-        for (int f = wave; f < MT * RT; f += PW) {
-            floatx4 sum = part[0][f][lane];
+            for (int i = 0; i < RT; ++i) acc[i] = mfma_chunk<T>(fv[u][i], xv[u], acc[i]);
+    }
+    for (; k < k_end; k += STEP) {
+        const u32x4 xv = load_chunk(x, k, k_end - CE * quad);
 #pragma unroll
-            for (int w = 1; w < PW; ++w) sum += part[w][f][lane];
-            const int t = 16 * (f / RT) + l16, r = r0 + 16 * (f % RT) + 4 * quad;
-            if (t < 32 && (now >> t & 1)) {
+        for (int i = 0; i < RT; ++i) acc[i] = mfma_chunk<T>(load_chunk(f[i], k, k_end - CE * quad), xv, acc[i]);
+    }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float h = r + i < rank ? s * sum[i] : 0.f;
-                    if (r + i < p.pitch) {
-                        p.H[(t0 + t) * p.pitch + r + i] = h;
-                        if (p.Hx) {
-                            uint16_t* const at = p.Hx + (t0 + t) * 2 * p.pitch + term_at(r + i);
-                            two_terms(h, at[0], at[16]);
-                        }
-                    }
-                    if (p.H_out && r + i < rows.rank) p.H_out[(t0 + t) * rows.rank + r + i] = h;
-                }
-            }
-        }
-        __syncthreads();
+    for (int i = 0; i < RT; ++i) part[wave][i][lane] = acc[i];
+    __syncthreads();
+    if (wave >= RT) return;
+    // wavefront i: factors 16 i ..; register e of lane (q, c): factor 4 q + e, row c
+    floatx4 sum = part[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < PW; ++w) sum += part[w][wave][lane];
+    if (l16 >= n_rows) return;
+    const float s = rows.scale ? rows.scale[a] : 1.f;
+    const int64_t t = t0 + l16;
+    const int r = r0 + 16 * wave + 4 * quad;
+    if (r >= p.pitch) return;
+    float h[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = r + e < rank ? s * sum[e] : 0.f;
+    *reinterpret_cast<floatx4*>(p.H + t * p.pitch + r) = floatx4{h[0], h[1], h[2], h[3]};
+    if (p.Hx) {
+        uint16_t first[4], second[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) two_terms(h[e], first[e], second[e]);
+        uint16_t* const at = p.Hx + t * 2 * p.pitch + term_at(r);
+        *reinterpret_cast<u32x2*>(at) = u32x2{(uint32_t)first[0] | (uint32_t)first[1] << 16, (uint32_t)first[2] | (uint32_t)first[3] << 16};
+        *reinterpret_cast<u32x2*>(at + 16) = u32x2{(uint32_t)second[0] | (uint32_t)second[1] << 16, (uint32_t)second[2] | (uint32_t)second[3] << 16};
+    }
+    if (p.H_out) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (r + e < rows.rank) p.H_out[t * rows.rank + r + e] = h[e];
     }
 }
 
 // A thread: 16 bytes of one row of the output.
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(256) void adapter_join_kernel(AdapterJoinArgs p, int blocks_n, int64_t t0)
 {
     constexpr int CE = 16 / (int)sizeof(T);
@@ -216,20 +229,14 @@ __global__ __launch_bounds__(256) void adapter_join_kernel(AdapterJoinArgs p, in
     for (int e = 0; e < CE; ++e) v[e] = 0.f;
     for (int s = 0; s < p.split; ++s) {
         const float* src = p.planes + ((int64_t)s * p.T + t) * p.N + n;
-        if (VEC) {
 #pragma unroll
-            for (int e = 0; e < CE; e += 4) {
-                const floatx4 x = *reinterpret_cast<const floatx4*>(src + e);
+        for (int e = 0; e < CE; e += 4) {
+            const u32x4 x = load_chunk(src, e, live);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[e + i] += x[i];
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < CE; ++e)
-                if (e < live) v[e] += src[e];
+            for (int i = 0; i < 4; ++i) v[e + i] += __uint_as_float((uint32_t)x[i]);
         }
     }
-    if (a >= 0) {
+    if (a >= 0 && a < p.count) {
         const int rank = rank_of(p.ranks, p.rank, a);
         const T* F = static_cast<const T*>(p.F) + (int64_t)a * p.rank * p.N + n;
         const float* h = p.H + t * adapter_pitch(p.rank);
@@ -239,7 +246,7 @@ __global__ __launch_bounds__(256) void adapter_join_kernel(AdapterJoinArgs p, in
 #pragma unroll 4
         for (int r = 0; r < rank; ++r) {
             const float hr = h[r];
-            const u32x4 f = load_chunk<T, VEC>(F + r * p.N, 0, live);
+            const u32x4 f = load_chunk(F + r * p.N, 0, live);
 #pragma unroll
             for (int e = 0; e < CE; ++e) {
                 const uint32_t w = f[sizeof(T) == 2 ? e >> 1 : e];
@@ -255,8 +262,8 @@ __global__ __launch_bounds__(256) void adapter_join_kernel(AdapterJoinArgs p, in
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
         *reinterpret_cast<u32x4*>(out) = o;
-    } else if (VEC) {
-        *reinterpret_cast<floatx4*>(out) = floatx4{v[0], v[1], v[2], v[3]};
+    } else if (live == CE) {
+        *reinterpret_cast<u32x4_by_word*>(out) = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
     } else {
 #pragma unroll
         for (int e = 0; e < CE; ++e)
@@ -279,10 +286,10 @@ struct OuterParams {
 // A tile of 16 CE columns and 16 RT factors of one block's gradient.  The workgroup lists the block's rows (WINDOW rows of the
 // matrix at a time), its wavefronts take four of them at a time: the fp32 MFMA's k.  Both operands come from memory in the
 // lanes' own order: lane (q, c) loads 16 bytes of row q, columns CE c .. , which are the columns CE c + f of MFMA f.
-template <typename T, bool VEC, int RT>
+template <typename T, int RT>
 __global__ __launch_bounds__(64 * OW) void adapter_outer_kernel(OuterParams p)
 {
-    constexpr int CE = 16 / (int)sizeof(T), U = 2;
+    constexpr int CE = 16 / (int)sizeof(T), U = RT == 1 ? 8 : 4;
     __shared__ int32_t list[WINDOW];
     __shared__ int counts[OW];
     __shared__ floatx4 part[OW][CE][64];
@@ -342,7 +349,7 @@ __global__ __launch_bounds__(64 * OW) void adapter_outer_kernel(OuterParams p)
                 const bool in = i < total;
                 const int64_t t = w0 + list[in ? i : 0];
                 g[u] = u32x4{0u, 0u, 0u, 0u};
-                if (in) g[u] = load_chunk<T, VEC>(static_cast<const T*>(sum.G) + t * sum.C, c0, sum.C);
+                if (in) g[u] = load_chunk(static_cast<const T*>(sum.G) + t * sum.C, c0, sum.C);
 #pragma unroll
                 for (int f = 0; f < RT; ++f) {
                     const int r = r0 + 16 * f + l16;
@@ -381,38 +388,34 @@ __global__ __launch_bounds__(64 * OW) void adapter_outer_kernel(OuterParams p)
     }
 }
 
-template <typename T, bool VEC, int RT>
-hipError_t project_rows(const ProjectParams& p, int rows, hipStream_t stream)
+template <typename T>
+hipError_t project_rank(const ProjectParams& p, hipStream_t stream)
 {
-    const unsigned y = (unsigned)std::max(1, (p.pitch + 16 * RT - 1) / (16 * RT));
-    const int64_t x = (p.rows.T + rows - 1) / rows;
-    if (x > MAX_BLOCKS) return hipErrorInvalidConfiguration;
-    if (rows == 1)
-        adapter_project_kernel<T, VEC, RT, 1><<<dim3((unsigned)x, y), 64 * PW, 0, stream>>>(p);
+    const int64_t windows = (p.rows.T + 15) / 16, blocks = windows + p.rows.requests;
+    if (blocks > MAX_BLOCKS) return hipErrorInvalidConfiguration;
+    const int rt = p.pitch <= 16 ? 1 : p.pitch <= 32 ? 2 : 4;
+    const dim3 grid((unsigned)blocks, (unsigned)std::max(1, (p.pitch + 16 * rt - 1) / (16 * rt)));
+    if (rt == 1)
+        adapter_project_kernel<T, 1><<<grid, 64 * PW, 0, stream>>>(p, (unsigned)windows);
+    else if (rt == 2)
+        adapter_project_kernel<T, 2><<<grid, 64 * PW, 0, stream>>>(p, (unsigned)windows);
     else
-        adapter_project_kernel<T, VEC, RT, 32><<<dim3((unsigned)x, y), 64 * PW, 0, stream>>>(p);
+        adapter_project_kernel<T, 4><<<grid, 64 * PW, 0, stream>>>(p, (unsigned)windows);
     return hipGetLastError();
 }
-template <typename T, bool VEC>
-hipError_t project_rank(const ProjectParams& p, int rows, hipStream_t stream)
-{
-    if (p.pitch <= 16) return project_rows<T, VEC, 1>(p, rows, stream);
-    if (p.pitch <= 32) return project_rows<T, VEC, 2>(p, rows, stream);
-    return project_rows<T, VEC, 4>(p, rows, stream);
-}
 
-template <typename T, bool VEC>
+template <typename T>
 hipError_t outer_rank(const OuterParams& p, hipStream_t stream)
 {
     const int rt = p.rank <= 16 ? 1 : p.rank <= 32 ? 2 : 4;
     const int64_t blocks = (int64_t)p.tiles * p.count * ((p.rank + 16 * rt - 1) / (16 * rt));
     if (blocks > MAX_BLOCKS) return hipErrorInvalidConfiguration;
     if (rt == 1)
-        adapter_outer_kernel<T, VEC, 1><<<(unsigned)blocks, 64 * OW, 0, stream>>>(p);
+        adapter_outer_kernel<T, 1><<<(unsigned)blocks, 64 * OW, 0, stream>>>(p);
     else if (rt == 2)
-        adapter_outer_kernel<T, VEC, 2><<<(unsigned)blocks, 64 * OW, 0, stream>>>(p);
+        adapter_outer_kernel<T, 2><<<(unsigned)blocks, 64 * OW, 0, stream>>>(p);
     else
-        adapter_outer_kernel<T, VEC, 4><<<(unsigned)blocks, 64 * OW, 0, stream>>>(p);
+        adapter_outer_kernel<T, 4><<<(unsigned)blocks, 64 * OW, 0, stream>>>(p);
     return hipGetLastError();
 }
 
@@ -422,10 +425,7 @@ hipError_t launch_adapter_project(const AdapterProjectArgs& a, DeviceInfo&, hipS
 {
     if (a.rows.T <= 0) return hipSuccess;
     ProjectParams p = {a.rows, a.X, a.F, a.K, a.row_adapter, a.H, a.H_out, a.Hx, adapter_pitch(a.rows.rank)};
-    // A tile of rows is gone through once for every block in it: rows of requests of a few tokens go one by one.
-    const int rows = a.rows.requests * 8 > a.rows.T ? 1 : 32;
-    if (a.bf16) return project_rank<uint16_t, true>(p, rows, stream);
-    return a.K % 4 == 0 ? project_rank<float, true>(p, rows, stream) : project_rank<float, false>(p, rows, stream);
+    return a.bf16 ? project_rank<uint16_t>(p, stream) : project_rank<float>(p, stream);
 }
 
 hipError_t launch_adapter_join(const AdapterJoinArgs& a, hipStream_t stream)
@@ -437,11 +437,9 @@ hipError_t launch_adapter_join(const AdapterJoinArgs& a, hipStream_t stream)
     for (int64_t t0 = 0; t0 < a.T; t0 += rows) {
         const unsigned blocks = (unsigned)(std::min(rows, a.T - t0) * blocks_n);
         if (a.bf16)
-            adapter_join_kernel<uint16_t, true><<<blocks, 256, 0, stream>>>(a, blocks_n, t0);
-        else if (a.N % 4 == 0)
-            adapter_join_kernel<float, true><<<blocks, 256, 0, stream>>>(a, blocks_n, t0);
+            adapter_join_kernel<uint16_t><<<blocks, 256, 0, stream>>>(a, blocks_n, t0);
         else
-            adapter_join_kernel<float, false><<<blocks, 256, 0, stream>>>(a, blocks_n, t0);
+            adapter_join_kernel<float><<<blocks, 256, 0, stream>>>(a, blocks_n, t0);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -462,8 +460,7 @@ hipError_t launch_adapter_outer(const AdapterOuterArgs& a, hipStream_t stream)
     p.T = a.T;
     p.tiles0 = (unsigned)((a.sum[0].C + width - 1) / width);
     p.tiles = p.tiles0 + (unsigned)((a.sum[1].C + width - 1) / width);
-    if (a.bf16) return outer_rank<uint16_t, true>(p, stream);
-    return a.sum[0].C % 4 == 0 && a.sum[1].C % 4 == 0 ? outer_rank<float, true>(p, stream) : outer_rank<float, false>(p, stream);
+    return a.bf16 ? outer_rank<uint16_t>(p, stream) : outer_rank<float>(p, stream);
 }
 
 }  // namespace sfb

@@ -45,7 +45,7 @@ struct BaseParams {
     const float* H;            // [M][adapter_pitch(rank)]
     const uint16_t* F;         // [count][rank][N]
     const int32_t* ranks;
-    int rank;
+    int count, rank;
     int tiles_m, tiles_n, group_m, num_xcd;
 };
 
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
         for (int i = 0; i < TBM / 64; ++i) {
             const int64_t m = m0 + 64 * i + lane;
             block[i] = m < p.M ? p.row_adapter[m] : ROW_OUTSIDE;
-            left[i] = __builtin_amdgcn_ballot_w64(block[i] >= 0);
+            left[i] = __builtin_amdgcn_ballot_w64(block[i] >= 0 && block[i] < p.count);
         }
         const int pitch = adapter_pitch(p.rank);
         const uint16_t* const hx = p.Hx + (m0 + wm0 + l16) * (2 * pitch) + 8 * quad;
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
         for (int k = 0; k < TM * TN / 2; ++k) {
             const int64_t m = m0 + wm0 + 16 * (k / (TN / 2)) + l16, n = n0 + wn0 + 32 * (k % (TN / 2)) + 8 * quad;
             const int a = m < p.M && n < p.N ? p.row_adapter[m] : ROW_OUTSIDE;
-            if (a < 0) continue;
+            if (a < 0 || a >= p.count) continue;
             int rank = p.ranks ? p.ranks[a] : p.rank;
             rank = rank < p.rank ? rank : p.rank;
             uint16_t* const out = p.out + m * p.N + n;
@@ -529,6 +529,7 @@ hipError_t launch_adapter_base_bf16(const AdapterBase& a, DeviceInfo& dev, hipSt
     p.H = a.H;
     p.F = a.F;
     p.ranks = a.ranks;
+    p.count = (int)a.count;
     p.rank = a.rank;
     p.num_xcd = dev.xcds > 0 ? dev.xcds : 1;
     const int64_t big = ((a.M + 255) / 256) * ((a.N + 255) / 256);

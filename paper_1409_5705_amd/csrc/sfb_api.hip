@@ -1111,6 +1111,7 @@ static int adapter_output(sfb_ctx* ctx, const AdapterLayout& l, const void* src,
         b.H = H;
         b.F = static_cast<const uint16_t*>(factors);
         b.ranks = ad->ranks;
+        b.count = ad->count;
         b.rank = ad->rank;
         SFB_RUN(KID_ADAPTER_BASE, sfb::launch_adapter_base_bf16(b, ctx->dev, ctx->stream));
         if (l.split == 1) return SFB_OK;
@@ -1135,6 +1136,7 @@ static int adapter_output(sfb_ctx* ctx, const AdapterLayout& l, const void* src,
     j.H = H;
     j.F = factors;
     j.ranks = ad->ranks;
+    j.count = ad->count;
     j.rank = ad->rank;
     j.out = out;
     j.bf16 = bf16;
