@@ -94,8 +94,11 @@ struct AdapterOuterArgs {
     int rank;
     bool bf16;
     int64_t T;
+    float* partial;            // with adapter_outer_splits > 1: so many times the size of both outputs
 };
 hipError_t launch_adapter_outer(const AdapterOuterArgs& a, hipStream_t stream);
+// Parts that the rows are divided into, C0 and C1 the columns of the two sums.
+int adapter_outer_splits(int64_t C0, int64_t C1, int64_t count, int rank, bool bf16, int64_t T);
 
 // Norm over the tensors of a list and their scaling.  partial: grad_norm_partials(...) + 1 doubles.  Where launch_clip follows
 // (clip), with the same list and `partial`, it may be that which writes *norm.

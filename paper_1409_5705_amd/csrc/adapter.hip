@@ -102,15 +102,14 @@ __device__ __forceinline__ void two_terms(float v, uint16_t& first, uint16_t& se
 __device__ __forceinline__ int term_at(int r) { return (r >> 4) * 32 + (r & 15); }
 
 constexpr int64_t MAX_BLOCKS = 1 << 22;      // workgroups of a launch (threads of a grid are counted in 32 bits)
-constexpr int PW = 16;      // wavefronts that share k
 
 // Up to 16 rows of one request against the 16 RT factors 16 RT * blockIdx.y ..; the wavefronts share k.  Workgroup w < windows
 // takes the rows from 16 w on, workgroup windows + q those from the first row of request q on, both to the next multiple of 16
 // or to the end of their request: every row once, and never two blocks in a workgroup.  (Tiles of 32 rows whatever the requests,
 // gone through once for every block in them: 8192 rows in 24 requests, K = 4096, 64 pairs 62 us.)
 // What bounds it is the stream of X: a wavefront's loads of U k-steps are in flight together.
-template <typename T, int RT>
-__global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams p, unsigned windows)
+template <typename T, int RT, int PW>
+__global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams p, unsigned windows, unsigned xcds)
 {
     constexpr int CE = 16 / (int)sizeof(T), STEP = 4 * CE, U = RT == 1 ? 8 : 4;
     __shared__ floatx4 part[PW][RT][64];
@@ -119,14 +118,21 @@ __global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams 
     const int r0 = (int)blockIdx.y * 16 * RT;
     const AdapterRows& rows = p.rows;
     int64_t t0, q;
-    if (blockIdx.x < windows) {
-        t0 = (int64_t)blockIdx.x * 16;
+    // neighbours, which are likely to use the same factors, go to the same XCD
+    unsigned tile = blockIdx.x;
+    {
+        const unsigned first = tile < windows ? 0 : windows, count = first ? gridDim.x - windows : windows;
+        const unsigned whole = count / xcds * xcds, i = tile - first;
+        if (i < whole) tile = first + i % xcds * (whole / xcds) + i / xcds;
+    }
+    if (tile < windows) {
+        t0 = (int64_t)tile * 16;
         const int64_t t = t0 + tid;
         if (tid < 16 && blockIdx.y == 0 && t < rows.T && (t < rows.start[0] || t >= rows.start[rows.requests])) p.row_adapter[t] = ROW_OUTSIDE;
         q = request_of(rows.start, rows.requests, t0, lane);
         if (q < 0) return;
     } else {
-        q = blockIdx.x - windows;
+        q = tile - windows;
         t0 = rows.start[q];
         if (t0 < 0 || t0 >= rows.T || (t0 & 15) == 0) return;
     }
@@ -279,18 +285,19 @@ struct OuterParams {
     const int32_t* ranks;
     int64_t count;
     int rank;
-    int64_t T;
+    int64_t T, per;            // rows, rows of a split
     unsigned tiles0, tiles;
+    float* partial;            // with splits: [split][count][rank][C of the first + C of the second]
 };
 
-// A tile of 16 CE columns and 16 RT factors of one block's gradient.  The workgroup lists the block's rows (WINDOW rows of the
-// matrix at a time), its wavefronts take four of them at a time: the fp32 MFMA's k.  Both operands come from memory in the
+// A tile of 16 CE columns and 16 RT factors of one block's gradient, over `per` rows of the matrix.  The workgroup lists the
+// block's rows (WINDOW rows of the matrix at a time), its wavefronts take four of them at a time: the fp32 MFMA's k.  Both operands come from memory in the
 // lanes' own order: lane (q, c) loads 16 bytes of row q, columns CE c .. , which are the columns CE c + f of MFMA f.
 template <typename T, int RT>
-__global__ __launch_bounds__(64 * OW) void adapter_outer_kernel(OuterParams p)
+__global__ __launch_bounds__(64 * OW, RT == 4 ? 2 : 4) void adapter_outer_kernel(OuterParams p)
 {
     constexpr int CE = 16 / (int)sizeof(T), U = RT == 1 ? 8 : 4;
-    __shared__ int32_t list[WINDOW];
+    __shared__ uint16_t list[WINDOW];
     __shared__ int counts[OW];
     __shared__ floatx4 part[OW][CE][64];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
@@ -307,7 +314,8 @@ __global__ __launch_bounds__(64 * OW) void adapter_outer_kernel(OuterParams p)
     for (int f = 0; f < RT; ++f)
 #pragma unroll
         for (int e = 0; e < CE; ++e) acc[f][e] = floatx4{0.f, 0.f, 0.f, 0.f};
-    for (int64_t w0 = 0; w0 < p.T && r0 < rank; w0 += WINDOW) {
+    const int64_t t_begin = (int64_t)blockIdx.y * p.per, t_end = t_begin + p.per < p.T ? t_begin + p.per : p.T;
+    for (int64_t w0 = t_begin; w0 < t_end && r0 < rank; w0 += WINDOW) {
         // the rows of the window that belong to the block, in their order
         constexpr int PER = WINDOW / (64 * OW);
         int found = 0;
@@ -315,7 +323,7 @@ __global__ __launch_bounds__(64 * OW) void adapter_outer_kernel(OuterParams p)
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int64_t t = w0 + tid * PER + i;
-            if (t < p.T && p.row_adapter[t] == a) {
+            if (t < t_end && p.row_adapter[t] == a) {
                 bits |= 1u << i;
                 ++found;
             }
@@ -338,7 +346,7 @@ __global__ __launch_bounds__(64 * OW) void adapter_outer_kernel(OuterParams p)
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            if (bits >> i & 1) list[before++] = tid * PER + i;
+            if (bits >> i & 1) list[before++] = (uint16_t)(tid * PER + i);
         __syncthreads();
         for (int i0 = wave * 4 * U; i0 < total; i0 += OW * 4 * U) {
             u32x4 g[U];
@@ -368,6 +376,9 @@ __global__ __launch_bounds__(64 * OW) void adapter_outer_kernel(OuterParams p)
         }
         __syncthreads();
     }
+    float* const out = p.partial ? p.partial + ((int64_t)blockIdx.y * p.count + a) * p.rank * (p.sum[0].C + p.sum[1].C) +
+                                       (tile >= p.tiles0 ? p.rank * p.sum[0].C : 0)
+                                 : sum.out + (int64_t)a * p.rank * sum.C;
     // register i of lane (q, c): factor 4 q + i, column CE c + e of acc[.][e]
 #pragma unroll
     for (int f = 0; f < RT; ++f) {
@@ -381,51 +392,85 @@ __global__ __launch_bounds__(64 * OW) void adapter_outer_kernel(OuterParams p)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = r0 + 16 * f + 4 * quad + i;
-                if (r < p.rank && c0 + e < sum.C) sum.out[((int64_t)a * p.rank + r) * sum.C + c0 + e] = r < rank ? s[i] : 0.f;
+                if (r < p.rank && c0 + e < sum.C) out[(int64_t)r * sum.C + c0 + e] = r < rank ? s[i] : 0.f;
             }
         }
         __syncthreads();
     }
 }
 
+// Adds the splits' sums up, in their order.
+__global__ __launch_bounds__(256) void adapter_outer_join_kernel(OuterParams p, int splits)
+{
+    const int64_t first = p.rank * p.sum[0].C, all = first + p.rank * p.sum[1].C, total = p.count * all;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        float v = p.partial[i];
+        for (int s = 1; s < splits; ++s) v += p.partial[s * total + i];
+        const int64_t a = i / all, at = i % all;
+        if (at < first)
+            p.sum[0].out[a * first + at] = v;
+        else
+            p.sum[1].out[a * (all - first) + at - first] = v;
+    }
+}
+
+template <typename T, int RT>
+void project_start(const ProjectParams& p, dim3 grid, unsigned windows, const DeviceInfo& dev, hipStream_t stream)
+{
+    const unsigned xcds = dev.xcds > 0 ? dev.xcds : 1;
+    // few workgroups: 16 wavefronts share k, and all of a row is on its way at once; many: eight, and two or three workgroups a
+    // CU hide each other's start (8192 rows, K = 4096, 16 pairs: 30 us with 16, 27 with 8)
+    if ((int64_t)grid.x * grid.y < dev.cus)
+        adapter_project_kernel<T, RT, 16><<<grid, 64 * 16, 0, stream>>>(p, windows, xcds);
+    else
+        adapter_project_kernel<T, RT, 8><<<grid, 64 * 8, 0, stream>>>(p, windows, xcds);
+}
 template <typename T>
-hipError_t project_rank(const ProjectParams& p, hipStream_t stream)
+hipError_t project_rank(const ProjectParams& p, const DeviceInfo& dev, hipStream_t stream)
 {
     const int64_t windows = (p.rows.T + 15) / 16, blocks = windows + p.rows.requests;
     if (blocks > MAX_BLOCKS) return hipErrorInvalidConfiguration;
     const int rt = p.pitch <= 16 ? 1 : p.pitch <= 32 ? 2 : 4;
     const dim3 grid((unsigned)blocks, (unsigned)std::max(1, (p.pitch + 16 * rt - 1) / (16 * rt)));
     if (rt == 1)
-        adapter_project_kernel<T, 1><<<grid, 64 * PW, 0, stream>>>(p, (unsigned)windows);
+        project_start<T, 1>(p, grid, (unsigned)windows, dev, stream);
     else if (rt == 2)
-        adapter_project_kernel<T, 2><<<grid, 64 * PW, 0, stream>>>(p, (unsigned)windows);
+        project_start<T, 2>(p, grid, (unsigned)windows, dev, stream);
     else
-        adapter_project_kernel<T, 4><<<grid, 64 * PW, 0, stream>>>(p, (unsigned)windows);
+        project_start<T, 4>(p, grid, (unsigned)windows, dev, stream);
     return hipGetLastError();
 }
 
-template <typename T>
-hipError_t outer_rank(const OuterParams& p, hipStream_t stream)
+int outer_rt(int rank) { return rank <= 16 ? 1 : rank <= 32 ? 2 : 4; }
+int64_t outer_blocks(int64_t C0, int64_t C1, int64_t count, int rank, bool bf16)
 {
-    const int rt = p.rank <= 16 ? 1 : p.rank <= 32 ? 2 : 4;
-    const int64_t blocks = (int64_t)p.tiles * p.count * ((p.rank + 16 * rt - 1) / (16 * rt));
-    if (blocks > MAX_BLOCKS) return hipErrorInvalidConfiguration;
+    const int64_t width = 16 * (bf16 ? 8 : 4), rt = outer_rt(rank);
+    return ((C0 + width - 1) / width + (C1 + width - 1) / width) * count * ((rank + 16 * rt - 1) / (16 * rt));
+}
+
+template <typename T>
+hipError_t outer_rank(const OuterParams& p, int splits, hipStream_t stream)
+{
+    const int rt = outer_rt(p.rank);
+    const int64_t workgroups = (int64_t)p.tiles * p.count * ((p.rank + 16 * rt - 1) / (16 * rt));
+    if (workgroups > MAX_BLOCKS) return hipErrorInvalidConfiguration;
+    const dim3 blocks((unsigned)workgroups, (unsigned)splits);
     if (rt == 1)
-        adapter_outer_kernel<T, 1><<<(unsigned)blocks, 64 * OW, 0, stream>>>(p);
+        adapter_outer_kernel<T, 1><<<blocks, 64 * OW, 0, stream>>>(p);
     else if (rt == 2)
-        adapter_outer_kernel<T, 2><<<(unsigned)blocks, 64 * OW, 0, stream>>>(p);
+        adapter_outer_kernel<T, 2><<<blocks, 64 * OW, 0, stream>>>(p);
     else
-        adapter_outer_kernel<T, 4><<<(unsigned)blocks, 64 * OW, 0, stream>>>(p);
+        adapter_outer_kernel<T, 4><<<blocks, 64 * OW, 0, stream>>>(p);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_adapter_project(const AdapterProjectArgs& a, DeviceInfo&, hipStream_t stream)
+hipError_t launch_adapter_project(const AdapterProjectArgs& a, DeviceInfo& dev, hipStream_t stream)
 {
     if (a.rows.T <= 0) return hipSuccess;
     ProjectParams p = {a.rows, a.X, a.F, a.K, a.row_adapter, a.H, a.H_out, a.Hx, adapter_pitch(a.rows.rank)};
-    return a.bf16 ? project_rank<uint16_t>(p, stream) : project_rank<float>(p, stream);
+    return a.bf16 ? project_rank<uint16_t>(p, dev, stream) : project_rank<float>(p, dev, stream);
 }
 
 hipError_t launch_adapter_join(const AdapterJoinArgs& a, hipStream_t stream)
@@ -446,6 +491,14 @@ hipError_t launch_adapter_join(const AdapterJoinArgs& a, hipStream_t stream)
     return hipSuccess;
 }
 
+// Two workgroups a CU at least, of 512 rows of the matrix at least.
+int adapter_outer_splits(int64_t C0, int64_t C1, int64_t count, int rank, bool bf16, int64_t T)
+{
+    if (count <= 0 || T <= 0) return 1;
+    const int64_t blocks = outer_blocks(C0, C1, count, rank, bf16), s = std::min((512 + blocks - 1) / blocks, T / 512);
+    return s < 2 ? 1 : s > 16 ? 16 : (int)s;
+}
+
 hipError_t launch_adapter_outer(const AdapterOuterArgs& a, hipStream_t stream)
 {
     if (a.count <= 0) return hipSuccess;
@@ -460,7 +513,14 @@ hipError_t launch_adapter_outer(const AdapterOuterArgs& a, hipStream_t stream)
     p.T = a.T;
     p.tiles0 = (unsigned)((a.sum[0].C + width - 1) / width);
     p.tiles = p.tiles0 + (unsigned)((a.sum[1].C + width - 1) / width);
-    return a.bf16 ? outer_rank<uint16_t>(p, stream) : outer_rank<float>(p, stream);
+    const int splits = adapter_outer_splits(a.sum[0].C, a.sum[1].C, a.count, a.rank, a.bf16, a.T);
+    p.per = (a.T + splits - 1) / splits;
+    p.partial = splits > 1 ? a.partial : nullptr;
+    const hipError_t e = a.bf16 ? outer_rank<uint16_t>(p, splits, stream) : outer_rank<float>(p, splits, stream);
+    if (e != hipSuccess || splits == 1) return e;
+    const int64_t total = a.count * a.rank * (a.sum[0].C + a.sum[1].C);
+    adapter_outer_join_kernel<<<(unsigned)std::min<int64_t>((total + 255) / 256, 4096), 256, 0, stream>>>(p, splits);
+    return hipGetLastError();
 }
 
 }  // namespace sfb

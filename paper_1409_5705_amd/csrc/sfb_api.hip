@@ -1031,7 +1031,7 @@ static int check_adapters(int64_t J, int64_t D, int64_t T, const sfb_adapters* a
 // The workspace of either call: the block of each row, the projections (forward H; backward H and dH), the product with the
 // shared matrix (N columns, contracted over K) and what its contraction needs itself.
 struct AdapterLayout {
-    int64_t off_h, off_dh, off_terms, off_planes, off_partial, total;
+    int64_t off_h, off_dh, off_terms, off_planes, off_partial, off_outer, total;
     int split;      // 1 with bf16 blocks: one kernel makes the whole output
 };
 static AdapterLayout adapter_layout(int64_t T, int64_t N, int64_t K, const sfb_adapters* ad, bool backward)
@@ -1045,7 +1045,9 @@ static AdapterLayout adapter_layout(int64_t T, int64_t N, int64_t K, const sfb_a
     l.split = bf16 ? sfb::adapter_base_split(T, N, K) : 1;
     l.off_planes = l.off_terms + (bf16 ? h : 0);
     l.off_partial = l.off_planes + (bf16 && l.split == 1 ? 0 : round_up(l.split * T * N * 4));
-    l.total = l.off_partial + (!bf16 && T > 0 ? round_up(sfb::gemm_f32_partial_bytes(T, N, K)) : 0);
+    l.off_outer = l.off_partial + (!bf16 && T > 0 ? round_up(sfb::gemm_f32_partial_bytes(T, N, K)) : 0);
+    const int splits = backward && ad->count > 0 ? sfb::adapter_outer_splits(K, N, ad->count, ad->rank, bf16, T) : 1;
+    l.total = l.off_outer + (splits > 1 ? round_up(splits * ad->count * ad->rank * (N + K) * 4) : 0);
     return l;
 }
 
@@ -1124,7 +1126,7 @@ static int adapter_output(sfb_ctx* ctx, const AdapterLayout& l, const void* src,
         g.C = planes; g.ldc = N;
         g.M = T; g.N = N; g.K = K;
         g.epilogue = sfb::EPI_STORE;
-        if (l.total > l.off_partial) g.partial = reinterpret_cast<float*>(ctx->ws + l.off_partial);
+        if (l.off_outer > l.off_partial) g.partial = reinterpret_cast<float*>(ctx->ws + l.off_partial);
         g.parts = &parts;
         SFB_RUN(KID_ADAPTER_BASE, sfb::launch_gemm_f32(g, ctx->stream));
         if (parts > 1) {      // the join adds them up
@@ -1234,6 +1236,7 @@ int sfb_adapter_backward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J
     o.rank = ad->rank;
     o.bf16 = a.bf16;
     o.T = T;
+    o.partial = reinterpret_cast<float*>(ctx->ws + l.off_outer);
     SFB_RUN(KID_ADAPTER_OUTER, sfb::launch_adapter_outer(o, ctx->stream));
     return SFB_OK;
 }

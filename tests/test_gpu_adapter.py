@@ -74,6 +74,7 @@ CASES = [
     (515, 392, 72, 7, 100, 130, False, 0, 3),
     (700, 128, 640, 40, 5, 200, False, 0, 0),
     (1100, 520, 264, 1, 12, 1, False, 0, 0),
+    (2600, 264, 520, 2, 40, 7, False, 5, 9),
 ]
 
 
@@ -96,6 +97,16 @@ def test_forward_and_backward(ctx, case, dtype):
     forward(ctx, d, q, H=False)
     assert torch.equal(q["Y"], o["Y"])
     assert bool((q["H"] == SENTINEL).all())
+
+
+@pytest.mark.parametrize("J,D,n,R,S", [(4104, 72, 5, 24, 9), (72, 4104, 5, 24, 9), (4104, 136, 30, 70, 300), (200, 4360, 30, 70, 300)])
+def test_many_tiles(ctx, J, D, n, R, S):
+    """Outputs of more tiles than the chip has compute units, rows of no request in the first and in the last ones."""
+    c = A.poison(A.make(4200, J, D, n, R, S, BF16, seed=J + S, first=3, behind=260))
+    d, o = to_dev(c), outputs(c)
+    forward(ctx, d, o)
+    backward(ctx, d, o, H=o["H"])
+    compare(c, o)
 
 
 @pytest.mark.parametrize("J,D,n,R", [(1003, 2047, 2, 12), (65, 63, 3, 5), (2, 3, 2, 1), (130, 1, 1, 7)])
@@ -179,15 +190,16 @@ def test_block_is_what_apply_would_make(ctx, sfb):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("T,S", [(24, 24), (300, 12)])
-def test_what_is_not_finite_stays_in_its_row(ctx, dtype, T, S):
+@pytest.mark.parametrize("T,S,J,D", [(24, 24, 136, 200), (300, 12, 136, 200), (300, 12, 136, 40), (4200, 900, 4104, 40), (4200, 12, 40, 4104)])
+def test_what_is_not_finite_stays_in_its_row(ctx, dtype, T, S, J, D):
     """Infinities and not-a-numbers in one request's rows or block do not reach the rows of others."""
-    J, D, n, R = 136, 200, 4, 8
+    n, R = 4, 8
     c = A.make(T, J, D, n, R, S, dtype, seed=11, single=S == T, none=0)
     c["ranks"][:] = R
     c["adapter"] = (torch.arange(S) % n).to(torch.int32)
     ref, rows = A.reference(c)
-    bad = [t for t in range(T) if int(c["adapter"][max(q for q in range(S) if int(c["start"][q]) <= t)]) == 1]
+    by, _ = A.rows_of(c)
+    bad = by.get(1, [])
     good = sorted(set(rows) - set(bad))
     c["U"][1, 2, 5] = float("inf")
     c["V"][1, 3, 7] = float("nan")
