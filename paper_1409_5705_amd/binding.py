@@ -277,6 +277,8 @@ class Context:
             raise SfbError(rc, "sfb_create")
         self._ws = None
         self._captured, self._retired = False, []      # workspaces that captured graphs may still work in
+        self._index = self.device.index or 0
+        self._ad, self._rq, self._needs = sfb_adapters(), sfb_requests(), {}
         self._shadow = None          # (W tensor, buffer tensor)
 
     # -- bf16 working copy of W ----------------------------------------------
@@ -537,81 +539,88 @@ class Context:
         self._check(rc, "sfb_dual_to_primal_l2")
 
     # -- factor blocks beside a shared matrix -----------------------------------
-    def _here(self, **tensors):
-        for name, t in tensors.items():
-            if t is not None and t.device != self.device:
-                raise ValueError("%s must be on %s, got %s" % (name, self.device, t.device))
+    def _at(self, t, name, dtype, shape):
+        """_ptr of a tensor that has to be on the context's device."""
+        if (type(t) is torch.Tensor and t.is_cuda and t.get_device() == self._index and t.is_contiguous() and t.dtype is dtype
+                and t.shape == shape):
+            return t.data_ptr()
+        p = _ptr(t, name, dtype=dtype, shape=shape)
+        if p is None:
+            raise TypeError("%s is missing" % name)
+        if t.get_device() != self._index:
+            raise ValueError("%s must be on %s, got %s" % (name, self.device, t.device))
+        return p
 
     def _stream_workspace(self, need):
         """Room for `need` bytes, allocated on the context's stream.  What a captured graph works in stays allocated when the
         workspace grows: the graph replays on the old one."""
-        capturing = torch.cuda.is_current_stream_capturing()
+        capturing = torch._C._cuda_isCurrentStreamCapturing()
+        self._captured = self._captured or capturing
         if self._ws is None or need > self._ws.numel():
-            self._captured = self._captured or capturing
             if self._ws is not None and not self._captured:
                 self._ws.record_stream(self.stream)
             with torch.cuda.stream(self.stream):
                 self.sfb_set_workspace(torch.empty(need, dtype=torch.uint8, device=self.device))
-        self._captured = self._captured or capturing
+
+    def _adapter_workspace(self, query, J, D, T, ad):
+        key = (query, J, D, T, ad.count, ad.rank, ad.dtype)
+        need = self._needs.get(key)
+        if need is None:
+            need = int(getattr(lib(), query)(J, D, T, ctypes.byref(ad)))
+            if need < 0:
+                raise SfbError(need, query)
+            if len(self._needs) > 1000:
+                self._needs.clear()
+            self._needs[key] = need
+        self._stream_workspace(need)
 
     def _adapters(self, W, X, start, adapter, U, V, ranks, scale):
         J, D = W.shape
-        if U.dim() != 3 or V.dim() != 3 or X.dim() != 2:
+        T = X.shape[0]
+        if U.dim() != 3 or X.dim() != 2:
             raise ValueError("U and V must be [count][rank][...], X [T][D]")
-        n, R = U.shape[0], U.shape[1]
-        self._here(W=W, X=X, start=start, adapter=adapter, U=U, V=V, ranks=ranks, scale=scale)
-        ad, rq = sfb_adapters(), sfb_requests()
+        n, R, _ = U.shape
+        dtype, ad, rq, at = X.dtype, self._ad, self._rq, self._at
         ad.count, ad.rank, ad.dtype = n, R, _dtype_code(X)
-        ad.U = _ptr(U, "U", dtype=X.dtype, shape=(n, R, J))
-        ad.V = _ptr(V, "V", dtype=X.dtype, shape=(n, R, D))
-        ad.ranks = None if ranks is None else _ptr(ranks, "ranks", dtype=torch.int32, shape=(n,))
-        ad.scale = None if scale is None else _ptr(scale, "scale", dtype=torch.float32, shape=(n,))
+        ad.U = at(U, "U", dtype, (n, R, J))
+        ad.V = at(V, "V", dtype, (n, R, D))
+        ad.ranks = None if ranks is None else at(ranks, "ranks", torch.int32, (n,))
+        ad.scale = None if scale is None else at(scale, "scale", torch.float32, (n,))
         S = adapter.numel()
-        rq.start = _ptr(start, "start", dtype=torch.int64, shape=(S + 1,))
-        rq.adapter = _ptr(adapter, "adapter", dtype=torch.int32, shape=(S,))
+        rq.start = at(start, "start", torch.int64, (S + 1,))
+        rq.adapter = at(adapter, "adapter", torch.int32, (S,))
         rq.count = S
-        return J, D, X.shape[0], ad, rq
+        return J, D, T, n, R, dtype, ad, rq, at(W, "W", W.dtype, (J, D)), at(X, "X", dtype, (T, D))
 
     def sfb_adapter_forward(self, W, X, start, adapter, U, V, Y, ranks=None, scale=None, H=None):
         """Enqueues Y = X W^T + H U_a (H = scale_a X V_a^T, written too where a tensor for it is given): rows
         start[q] .. start[q + 1] - 1 of X [T][D] with the factor block a = adapter[q] of U [n][R][J], V [n][R][D] (outside
         [0, n): none).  start int64 [S + 1] and adapter int32 [S] on the device; rows of no request stay as they are."""
-        J, D, T, ad, rq = self._adapters(W, X, start, adapter, U, V, ranks, scale)
-        self._here(Y=Y, H=H)
-        need = lib().sfb_adapter_forward_workspace_bytes(J, D, T, ctypes.byref(ad))
-        if need < 0:
-            raise SfbError(int(need), "sfb_adapter_forward_workspace_bytes")
-        self._stream_workspace(int(need))
-        rc = lib().sfb_adapter_forward(self._h, _ptr(W, "W"), _dtype_code(W), J, D, _ptr(X, "X", shape=(T, D)), T, ctypes.byref(ad),
-                                       ctypes.byref(rq), _ptr(Y, "Y", dtype=X.dtype, shape=(T, J)),
-                                       None if H is None else _ptr(H, "H", dtype=torch.float32, shape=(T, ad.rank)))
+        J, D, T, n, R, dtype, ad, rq, Wp, Xp = self._adapters(W, X, start, adapter, U, V, ranks, scale)
+        self._adapter_workspace("sfb_adapter_forward_workspace_bytes", J, D, T, ad)
+        rc = lib().sfb_adapter_forward(self._h, Wp, _dtype_code(W), J, D, Xp, T, ad, rq, self._at(Y, "Y", dtype, (T, J)),
+                                       None if H is None else self._at(H, "H", torch.float32, (T, R)))
         self._check(rc, "sfb_adapter_forward")
 
     def sfb_adapter_backward(self, W, X, dY, start, adapter, U, V, dX=None, dU=None, dV=None, ranks=None, scale=None, H=None):
         """Enqueues the gradients of the forward call at dY [T][J]: dX of X's dtype, dU [n][R][J] and dV [n][R][D] fp32
         (None: not wanted).  H: what the forward call wrote, or None."""
-        J, D, T, ad, rq = self._adapters(W, X, start, adapter, U, V, ranks, scale)
-        self._here(dY=dY, dX=dX, dU=dU, dV=dV, H=H)
-        need = lib().sfb_adapter_backward_workspace_bytes(J, D, T, ctypes.byref(ad))
-        if need < 0:
-            raise SfbError(int(need), "sfb_adapter_backward_workspace_bytes")
-        self._stream_workspace(int(need))
-        n, R = ad.count, ad.rank
-        rc = lib().sfb_adapter_backward(self._h, _ptr(W, "W"), _dtype_code(W), J, D, _ptr(X, "X", shape=(T, D)),
-                                        _ptr(dY, "dY", dtype=X.dtype, shape=(T, J)), T, ctypes.byref(ad), ctypes.byref(rq),
-                                        None if H is None else _ptr(H, "H", dtype=torch.float32, shape=(T, R)),
-                                        None if dX is None else _ptr(dX, "dX", dtype=X.dtype, shape=(T, D)),
-                                        None if dU is None else _ptr(dU, "dU", dtype=torch.float32, shape=(n, R, J)),
-                                        None if dV is None else _ptr(dV, "dV", dtype=torch.float32, shape=(n, R, D)))
+        J, D, T, n, R, dtype, ad, rq, Wp, Xp = self._adapters(W, X, start, adapter, U, V, ranks, scale)
+        self._adapter_workspace("sfb_adapter_backward_workspace_bytes", J, D, T, ad)
+        at, f32 = self._at, torch.float32
+        rc = lib().sfb_adapter_backward(self._h, Wp, _dtype_code(W), J, D, Xp, at(dY, "dY", dtype, (T, J)), T, ad, rq,
+                                        None if H is None else at(H, "H", f32, (T, R)),
+                                        None if dX is None else at(dX, "dX", dtype, (T, D)),
+                                        None if dU is None else at(dU, "dU", f32, (n, R, J)),
+                                        None if dV is None else at(dV, "dV", f32, (n, R, D)))
         self._check(rc, "sfb_adapter_backward")
 
     # -- norm and clipping of gradients ------------------------------------------
     def _list(self, tensors, norm):
         if tensors.device is not None and tensors.device != self.device:
             raise ValueError("the tensors must be on %s, got %s" % (self.device, tensors.device))
-        self._here(norm=norm)
         self._stream_workspace(tensors.workspace_bytes)
-        return _ptr(norm, "norm", dtype=torch.float32, shape=(1,))
+        return self._at(norm, "norm", torch.float32, (1,))
 
     def sfb_grad_norm(self, tensors: TensorList, norm):
         """Enqueues norm[0] = the global 2-norm of the list's tensors."""

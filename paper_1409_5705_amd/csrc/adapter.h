@@ -62,12 +62,28 @@ struct AdapterBase {
 hipError_t launch_adapter_base_bf16(const AdapterBase& a, DeviceInfo& dev, hipStream_t stream);
 int adapter_base_split(int64_t M, int64_t N, int64_t K);
 
+// The same for few rows: planes alone, of `width` columns; with `dense` those behind the N of the product are A times the
+// factors of all blocks ([count][rank][K]).  row_adapter (nullable): written as launch_adapter_project does.
+constexpr int64_t FEW_ROWS = 128;
+struct AdapterFewPlan {
+    bool few = false, dense = false;
+    int split = 1;
+    int64_t width = 0;
+};
+AdapterFewPlan adapter_few_plan(int64_t M, int64_t N, int64_t K, int64_t factors);
+hipError_t launch_adapter_few(const AdapterBase& a, const AdapterFewPlan& plan, const AdapterRows& rows, int32_t* row_adapter, DeviceInfo& dev,
+                              hipStream_t stream);
+
 // out[t][n] = sum_s planes[s][t][n] + sum_r H[t][r] F_a[r][n] for the rows of requests; out and F [count][rank][N] fp32 or bf16.
 struct AdapterJoinArgs {
-    const float* planes;
+    const float* planes;       // [split][T][width]
+    int64_t width;
     int split;
     const int32_t* row_adapter;
-    const float* H;            // [T][adapter_pitch(rank)]
+    bool dense;                // H is made from the planes and written, otherwise read
+    float* H;                  // [T][adapter_pitch(rank)]
+    float* H_out;              // dense: nullable, [T][rank]
+    const float* scale;        // dense
     const void* F;
     const int32_t* ranks;
     int64_t count;

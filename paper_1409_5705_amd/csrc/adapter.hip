@@ -6,7 +6,7 @@
 //
 // Rows of one matrix belong to different blocks, so what one row holds (an infinity, a NaN) never meets another row's sum:
 // a product takes rows of ONE block at a time, and the others' results are dropped, not multiplied by zero.
-#include "adapter.h"
+#include "adapter_device.h"
 #include "device.h"
 
 #include <algorithm>
@@ -20,27 +20,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float bf16_float(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
-
-// The request of row t, or -1 (empty requests are passed over: the last q with start[q] <= t).  By a whole wavefront: 64
-// probes a step.
-__device__ __forceinline__ int64_t request_of(const int64_t* start, int64_t requests, int64_t t, int lane)
-{
-    if (requests <= 0 || t < start[0] || t >= start[requests]) return -1;
-    int64_t lo = 0, n = requests;                  // start[lo] <= t; the answer is in [lo, lo + n)
-    while (n > 1) {
-        const int64_t step = (n + 63) / 64, at = lane * step;
-        const uint64_t below = __builtin_amdgcn_ballot_w64(at < n && start[lo + at] <= t);
-        const int64_t k = 63 - __builtin_clzll(below | 1);
-        lo += k * step;
-        n = n - k * step < step ? n - k * step : step;
-    }
-    return lo;
-}
-__device__ __forceinline__ int rank_of(const int32_t* ranks, int rank, int64_t a)
-{
-    const int r = ranks ? ranks[a] : rank;
-    return r < 0 ? 0 : r < rank ? r : rank;
-}
 
 // 16 bytes of a row (eight bf16, four fp32).  fp32 rows need not be 16-byte aligned.
 typedef u32x4 u32x4_by_word __attribute__((aligned(4)));
@@ -221,58 +200,84 @@ __global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams 
     }
 }
 
-// A thread: 16 bytes of one row of the output.
+// A thread: four columns of one row of the output.  The row's projections come from H, or (dense) from the planes, which hold
+// the products with the factors of all blocks behind the columns of the output; then the first workgroup of a row stores them.
 template <typename T>
-__global__ __launch_bounds__(256) void adapter_join_kernel(AdapterJoinArgs p, int blocks_n, int64_t t0)
+__global__ __launch_bounds__(128) void adapter_join_kernel(AdapterJoinArgs p, int blocks_n, int64_t t0)
 {
-    constexpr int CE = 16 / (int)sizeof(T);
-    const int64_t t = t0 + blockIdx.x / blocks_n, n = ((int64_t)(blockIdx.x % blocks_n) * 256 + threadIdx.x) * CE;
+    __shared__ float h_of[256];
+    const int64_t t = t0 + blockIdx.x / blocks_n, n = ((int64_t)(blockIdx.x % blocks_n) * 128 + threadIdx.x) * 4;
+    const int live = p.N - n < 4 ? p.N - n < 0 ? 0 : (int)(p.N - n) : 4;
     const int a = p.row_adapter[t];
-    if (a == ROW_OUTSIDE || n >= p.N) return;
-    const int live = (int)(p.N - n < CE ? p.N - n : CE);
-    float v[CE];
+    floatx4 v = {0.f, 0.f, 0.f, 0.f};
+    const float* src = p.planes + t * p.width + n;
+    if (live == 4) {
+#pragma unroll 4
+        for (int s = 0; s < p.split; ++s) v += __builtin_bit_cast(floatx4, load_chunk(src + s * (p.T * p.width)));
+    } else {
+        for (int s = 0; s < p.split; ++s)
 #pragma unroll
-    for (int e = 0; e < CE; ++e) v[e] = 0.f;
-    for (int s = 0; s < p.split; ++s) {
-        const float* src = p.planes + ((int64_t)s * p.T + t) * p.N + n;
-#pragma unroll
-        for (int e = 0; e < CE; e += 4) {
-            const u32x4 x = load_chunk(src, e, live);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[e + i] += __uint_as_float((uint32_t)x[i]);
+            for (int e = 0; e < 4; ++e)
+                if (e < live) v[e] += src[s * (p.T * p.width) + e];
+    }
+    if (a == ROW_OUTSIDE) return;
+    const int pitch = adapter_pitch(p.rank);
+    const bool first = blockIdx.x % blocks_n == 0;
+    int rank = 0;
+    if (a >= 0 && a < p.count) {
+        rank = rank_of(p.ranks, p.rank, a);
+        const float scale = p.scale ? p.scale[a] : 1.f;
+        for (int r = threadIdx.x; r < rank; r += 128) {
+            float h;
+            if (p.dense) {
+                h = 0.f;
+                const float* from = p.planes + t * p.width + p.N + (int64_t)a * p.rank + r;
+                for (int s = 0; s < p.split; ++s) h += from[s * (p.T * p.width)];
+                h *= scale;
+            } else {
+                h = p.H[t * pitch + r];
+            }
+            h_of[r] = h;
+        }
+        __syncthreads();
+    }
+    if (p.dense && first) {
+        for (int r = threadIdx.x; r < pitch; r += 128) {
+            const float h = r < rank ? h_of[r] : 0.f;
+            p.H[t * pitch + r] = h;
+            if (p.H_out && r < p.rank) p.H_out[t * p.rank + r] = h;
         }
     }
-    if (a >= 0 && a < p.count) {
-        const int rank = rank_of(p.ranks, p.rank, a);
+    if (live == 0) return;
+    if (rank > 0) {
         const T* F = static_cast<const T*>(p.F) + (int64_t)a * p.rank * p.N + n;
-        const float* h = p.H + t * adapter_pitch(p.rank);
-        float low[CE];
-#pragma unroll
-        for (int e = 0; e < CE; ++e) low[e] = 0.f;
-#pragma unroll 4
+        floatx4 low = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
         for (int r = 0; r < rank; ++r) {
-            const float hr = h[r];
-            const u32x4 f = load_chunk(F + r * p.N, 0, live);
+            const float hr = h_of[r];
+            if constexpr (sizeof(T) == 2) {      // (N % 8 == 0: all four columns)
+                const u32x2 f = *reinterpret_cast<const u32x2*>(F + r * p.N);
 #pragma unroll
-            for (int e = 0; e < CE; ++e) {
-                const uint32_t w = f[sizeof(T) == 2 ? e >> 1 : e];
-                low[e] = fmaf(hr, __uint_as_float(sizeof(T) == 4 ? w : (e & 1) ? w & 0xffff0000u : w << 16), low[e]);
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t w = f[e >> 1];
+                    low[e] = fmaf(hr, __uint_as_float((e & 1) ? w & 0xffff0000u : w << 16), low[e]);
+                }
+            } else {
+                const u32x4 f = load_chunk(F + r * p.N, 0, live);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) low[e] = fmaf(hr, __uint_as_float((uint32_t)f[e]), low[e]);
             }
         }
-#pragma unroll
-        for (int e = 0; e < CE; ++e) v[e] += low[e];
+        v += low;
     }
     T* out = static_cast<T*>(p.out) + t * p.N + n;
     if constexpr (sizeof(T) == 2) {
-        u32x4 o;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-        *reinterpret_cast<u32x4*>(out) = o;
-    } else if (live == CE) {
-        *reinterpret_cast<u32x4_by_word*>(out) = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+        *reinterpret_cast<u32x2*>(out) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    } else if (live == 4) {
+        *reinterpret_cast<u32x4_by_word*>(out) = __builtin_bit_cast(u32x4, v);
     } else {
 #pragma unroll
-        for (int e = 0; e < CE; ++e)
+        for (int e = 0; e < 4; ++e)
             if (e < live) out[e] = v[e];
     }
 }
@@ -476,15 +481,14 @@ hipError_t launch_adapter_project(const AdapterProjectArgs& a, DeviceInfo& dev, 
 hipError_t launch_adapter_join(const AdapterJoinArgs& a, hipStream_t stream)
 {
     if (a.T <= 0) return hipSuccess;
-    const int ce = a.bf16 ? 8 : 4;
-    const int blocks_n = (int)((a.N + 256 * ce - 1) / (256 * ce));
+    const int blocks_n = (int)((a.N + 511) / 512);
     const int64_t rows = std::max<int64_t>(1, MAX_BLOCKS / blocks_n);
     for (int64_t t0 = 0; t0 < a.T; t0 += rows) {
         const unsigned blocks = (unsigned)(std::min(rows, a.T - t0) * blocks_n);
         if (a.bf16)
-            adapter_join_kernel<uint16_t><<<blocks, 256, 0, stream>>>(a, blocks_n, t0);
+            adapter_join_kernel<uint16_t><<<blocks, 128, 0, stream>>>(a, blocks_n, t0);
         else
-            adapter_join_kernel<float><<<blocks, 256, 0, stream>>>(a, blocks_n, t0);
+            adapter_join_kernel<float><<<blocks, 128, 0, stream>>>(a, blocks_n, t0);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

@@ -20,8 +20,10 @@
 // us backward (1.4 PFLOP/s).  What a tile costs besides its k-loop is instructions that are executed once, so their number
 // counts, and a register that is spilled around them more so (an earlier form with scratch memory and 80 KB of code: 30 us a
 // tile, this one 8).
-#include "adapter.h"
+#include "adapter_device.h"
 #include "planes.h"
+
+#include <algorithm>
 
 namespace sfb {
 namespace {
@@ -501,6 +503,143 @@ hipError_t launch_base(BaseParams& p, DeviceInfo& dev, hipStream_t stream)
     return hipGetLastError();
 }
 
+// ---- few rows ------------------------------------------------------------------------------------------------------------
+// The stream of W bounds the product of up to FEW_ROWS rows.  Tiles of 64 x 64 along a part of k, five LDS stages of a k-slice
+// each: 128 KB of requests of a CU's two workgroups in flight.  The blocks' factors are taken for further columns of the matrix:
+// every row is multiplied with the factors of all blocks (the matrix pipes have the time), and the join picks its own block's.
+struct FewParams {
+    const uint16_t* A;
+    const uint16_t* W;
+    const uint16_t* F;         // [factors][K]
+    int64_t M, N, K, ldw, pitch, factors, width;      // width: columns of a plane
+    float* planes;             // [split][M][width]
+    int split, tiles_m, tiles_w;
+    AdapterRows rows;
+    int32_t* row_adapter;      // nullable: written by the last workgroup
+};
+constexpr int NS = 5;
+
+template <bool TRANSPOSED>
+__global__ __launch_bounds__(256) void adapter_few_kernel(FewParams p)
+{
+    constexpr uint32_t TILE = 64 * 128, STAGE_BYTES = 2 * TILE;
+    extern __shared__ u32x4 smem[];
+    char* const lds = reinterpret_cast<char*>(smem);
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (p.row_adapter && blockIdx.x == gridDim.x - 1) {
+        if (blockIdx.y != 0) return;
+        const int64_t first = p.rows.start[0], last = p.rows.start[p.rows.requests];
+        for (int64_t t = tid; t < p.M; t += 256)
+            if (t < first || t >= last) p.row_adapter[t] = ROW_OUTSIDE;
+        for (int64_t q = tid; q < p.rows.requests; q += 256) {
+            int a = p.rows.adapter[q];
+            if (a < 0 || a >= p.rows.count || rank_of(p.rows.ranks, p.rows.rank, a) == 0) a = ROW_NONE;
+            const int64_t begin = p.rows.start[q], end = p.rows.start[q + 1];
+            for (int64_t t = begin < 0 ? 0 : begin; t < end && t < p.M; ++t) p.row_adapter[t] = a;
+        }
+        return;
+    }
+    const int wm0 = (wave >> 1) * 32, wn0 = (wave & 1) * 32;
+    const int64_t m0 = (int64_t)(blockIdx.x % (unsigned)p.tiles_m) * 64;
+    const int tile = (int)(blockIdx.x / (unsigned)p.tiles_m);
+    const bool factor = tile >= p.tiles_w;                 // columns of the blocks' factors, k-contiguous
+    const bool transposed = TRANSPOSED && !factor;
+    const int64_t n0 = (int64_t)(factor ? tile - p.tiles_w : tile) * 64;
+    const int64_t N = factor ? p.factors : p.N, ldw_e = factor ? p.K : p.ldw, pitch = factor ? 0 : p.pitch;
+    const uint16_t* const W = factor ? p.F : p.W;
+    const int slices = (int)((p.K + BK - 1) / BK);
+    const int s_begin = (int)((int64_t)slices * blockIdx.y / p.split), nk = (int)((int64_t)slices * (blockIdx.y + 1) / p.split) - s_begin;
+
+    const uint32_t lda = (uint32_t)p.K * 2u, ldw = pitch ? (uint32_t)BK * 2u : (uint32_t)ldw_e * 2u;
+    const int last_m = (int)(p.M - m0 < 64 ? p.M - m0 : 64), last_n = (int)(N - n0 < 64 ? N - n0 : 64);
+    uint32_t offA[2], offB[2];
+    int kA[2], kB[2];                                      // first k of what a lane loads
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = 8 * (2 * wave + i) + (lane >> 3), c = (lane & 7) ^ swz(r);
+        offA[i] = r < last_m ? (uint32_t)r * lda + (uint32_t)c * 16u : OUT_OF_RANGE;
+        kA[i] = 8 * c;
+        if (transposed) {
+            const int u = (lane & 7) ^ ((r & 1) << 2);     // LDS rows of 64 columns; chunk u of row r in slot u ^ 4 (r % 2)
+            offB[i] = 8 * u < last_n ? (uint32_t)r * ldw + (uint32_t)u * 16u : OUT_OF_RANGE;
+            kB[i] = r;
+        } else {
+            const int w = r & 31, n = r - w + column_of(w >> 4, w & 15);
+            offB[i] = n < last_n ? (uint32_t)n * ldw + (uint32_t)c * 16u : OUT_OF_RANGE;
+            kB[i] = 8 * c;
+        }
+    }
+    auto issue = [&](int s) {      // (past the last slice: nothing is in range)
+        const int64_t k0 = (int64_t)(s_begin + s) * BK;
+        const int left = s < nk ? (int)(p.K - k0 < BK ? p.K - k0 : BK) : 0;
+        const uint64_t at = transposed ? (pitch ? (uint64_t)(((k0 / BM) * (pitch / BK) + n0 / BK) * (BM * BK) + (k0 % BM) * BK) : (uint64_t)(k0 * ldw_e + n0))
+                                       : (pitch ? (uint64_t)(((n0 / BM) * (pitch / BK) + k0 / BK) * (BM * BK) + (n0 % BM) * BK) : (uint64_t)(n0 * ldw_e + k0));
+        const u32x4 ra = descriptor(reinterpret_cast<uint64_t>(p.A) + (uint64_t)(m0 * p.K + k0) * 2u);
+        const u32x4 rb = descriptor(reinterpret_cast<uint64_t>(W) + at * 2u);
+        const uint32_t dst = lds_base + (uint32_t)(s % NS) * STAGE_BYTES + (uint32_t)wave * 2048u;
+        buffer_to_lds_16<0>(dst, ra, kA[0] < left ? offA[0] : OUT_OF_RANGE);
+        buffer_to_lds_16<1024>(dst, ra, kA[1] < left ? offA[1] : OUT_OF_RANGE);
+        buffer_to_lds_16<TILE>(dst, rb, kB[0] < left ? offB[0] : OUT_OF_RANGE);
+        buffer_to_lds_16<TILE + 1024>(dst, rb, kB[1] < left ? offB[1] : OUT_OF_RANGE);
+    };
+    floatx4 acc[2][2];
+#pragma unroll
+    for (int ta = 0; ta < 2; ++ta)
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) acc[ta][tb] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < NS - 1; ++s) issue(s);
+    for (int s = 0; s < nk; ++s) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * (NS - 2)) : "memory");
+        __syncthreads();                                   // slice s is in LDS; every wavefront has read the slice before
+        issue(s + NS - 1);
+        const char* const stage = lds + (uint32_t)(s % NS) * STAGE_BYTES;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            bf16x8 a[2], b[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int r = wm0 + 16 * t + l16;
+                a[t] = *reinterpret_cast<const bf16x8*>(stage + r * 128 + (((4 * ks + quad) ^ swz(r)) << 4));
+            }
+            if (transposed) {
+                // lane i of a group: row i / 4 of four, piece i % 4 of the 32 columns of the wavefront
+                const int r = 32 * ks + 8 * quad + (l16 >> 2);
+                const char* const at = stage + TILE + r * 128 + ((((wn0 >> 3) + (l16 & 3)) ^ ((r & 1) << 2)) << 4);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * t));
+                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * t + 4 * 128));
+                    b[t] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const int r = wn0 + 16 * t + l16;
+                    b[t] = *reinterpret_cast<const bf16x8*>(stage + TILE + r * 128 + (((4 * ks + quad) ^ swz(r)) << 4));
+                }
+            }
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                for (int ta = 0; ta < 2; ++ta) acc[ta][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[tb], a[ta], acc[ta][tb], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int ta = 0; ta < 2; ++ta) {
+        const int64_t m = m0 + wm0 + 16 * ta + l16;
+        if (m >= p.M) continue;
+        float* const row = p.planes + ((int64_t)blockIdx.y * p.M + m) * p.width + (factor ? p.N : 0) + n0 + wn0;
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) {
+            const int n = column_of(tb, 4 * quad);
+            if (n0 + wn0 + n < N) *reinterpret_cast<floatx4*>(row + n) = acc[ta][tb];      // (a plane's row ends on a multiple of four)
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
 }  // namespace
 
 // Ways the contraction is divided along k: fewer tiles than half of what the chip holds at once, and at least four slices each.
@@ -510,6 +649,54 @@ int adapter_base_split(int64_t M, int64_t N, int64_t K)
     if (tiles <= 0 || tiles >= 256) return 1;
     const int64_t s = 512 / tiles < slices / 4 ? 512 / tiles : slices / 4;
     return s < 2 ? 1 : s > 16 ? 16 : (int)s;
+}
+
+AdapterFewPlan adapter_few_plan(int64_t M, int64_t N, int64_t K, int64_t factors)
+{
+    AdapterFewPlan f;
+    f.few = M > 0 && M <= FEW_ROWS;
+    if (!f.few) return f;
+    // the factors of the whole pool, or a launch of its own for those that are used: it takes as long as 16 MB of them
+    f.dense = factors * K <= (8 << 20);
+    f.width = N + (f.dense ? (factors + 3) / 4 * 4 : 0);
+    const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64 + (f.dense ? (factors + 63) / 64 : 0)), slices = (K + BK - 1) / BK;
+    const int64_t s = std::min(512 / tiles, slices / 6);
+    f.split = s < 1 ? 1 : s > 16 ? 16 : (int)s;
+    return f;
+}
+
+hipError_t launch_adapter_few(const AdapterBase& a, const AdapterFewPlan& plan, const AdapterRows& rows, int32_t* row_adapter, DeviceInfo& dev,
+                              hipStream_t stream)
+{
+    FewParams p = {};
+    p.A = a.A;
+    p.W = a.W;
+    p.F = a.F;
+    p.M = a.M; p.N = a.N; p.K = a.K;
+    p.ldw = a.transposed ? a.N : a.K;
+    p.pitch = a.blocked ? bf16_pitch(p.ldw) : 0;
+    p.factors = plan.dense ? rows.count * rows.rank : 0;
+    p.width = plan.width;
+    p.planes = a.planes;
+    p.split = plan.split;
+    p.tiles_m = (int)((a.M + 63) / 64);
+    p.tiles_w = (int)((a.N + 63) / 64);
+    p.rows = rows;
+    p.row_adapter = row_adapter;
+    constexpr int lds = NS * 2 * 64 * 128;
+    const void* const kernel = a.transposed ? reinterpret_cast<const void*>(&adapter_few_kernel<true>) : reinterpret_cast<const void*>(&adapter_few_kernel<false>);
+    bool& set = dev.adapter_few_lds_set[a.transposed ? 1 : 0];
+    if (!set) {
+        const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+        set = true;
+    }
+    const dim3 grid((unsigned)(p.tiles_m * (p.tiles_w + (p.factors + 63) / 64) + (row_adapter ? 1 : 0)), (unsigned)plan.split);
+    if (a.transposed)
+        adapter_few_kernel<true><<<grid, 256, lds, stream>>>(p);
+    else
+        adapter_few_kernel<false><<<grid, 256, lds, stream>>>(p);
+    return hipGetLastError();
 }
 
 hipError_t launch_adapter_base_bf16(const AdapterBase& a, DeviceInfo& dev, hipStream_t stream)

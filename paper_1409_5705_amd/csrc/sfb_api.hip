@@ -1032,7 +1032,9 @@ static int check_adapters(int64_t J, int64_t D, int64_t T, const sfb_adapters* a
 // shared matrix (N columns, contracted over K) and what its contraction needs itself.
 struct AdapterLayout {
     int64_t off_h, off_dh, off_terms, off_planes, off_partial, off_outer, total;
-    int split;      // 1 with bf16 blocks: one kernel makes the whole output
+    int split;      // 1 with bf16 blocks that are not few rows: one kernel makes the whole output
+    sfb::AdapterFewPlan few;
+    bool fused(bool bf16) const { return bf16 && split == 1 && !few.few; }
 };
 static AdapterLayout adapter_layout(int64_t T, int64_t N, int64_t K, const sfb_adapters* ad, bool backward)
 {
@@ -1042,9 +1044,10 @@ static AdapterLayout adapter_layout(int64_t T, int64_t N, int64_t K, const sfb_a
     l.off_dh = l.off_h + h;
     l.off_terms = l.off_dh + (backward ? h : 0);
     const bool bf16 = ad->dtype == SFB_BF16;
-    l.split = bf16 ? sfb::adapter_base_split(T, N, K) : 1;
+    if (bf16) l.few = sfb::adapter_few_plan(T, N, K, ad->count * ad->rank);
+    l.split = l.few.few ? l.few.split : bf16 ? sfb::adapter_base_split(T, N, K) : 1;
     l.off_planes = l.off_terms + (bf16 ? h : 0);
-    l.off_partial = l.off_planes + (bf16 && l.split == 1 ? 0 : round_up(l.split * T * N * 4));
+    l.off_partial = l.off_planes + (l.fused(bf16) ? 0 : round_up(l.split * T * (l.few.few ? l.few.width : N) * 4));
     l.off_outer = l.off_partial + (!bf16 && T > 0 ? round_up(sfb::gemm_f32_partial_bytes(T, N, K)) : 0);
     const int splits = backward && ad->count > 0 ? sfb::adapter_outer_splits(K, N, ad->count, ad->rank, bf16, T) : 1;
     l.total = l.off_outer + (splits > 1 ? round_up(splits * ad->count * ad->rank * (N + K) * 4) : 0);
@@ -1088,16 +1091,42 @@ static int check_adapter_call(const sfb_ctx* ctx, const void* W, int32_t w_dtype
     return SFB_OK;
 }
 
-// out = src times the shared matrix (transposed: by its columns) + H times the blocks' `factors`.
+static sfb::AdapterProjectArgs project_args(sfb_ctx* ctx, int64_t T, const sfb_adapters* ad, const sfb_requests* rq)
+{
+    sfb::AdapterProjectArgs a = {};
+    a.rows.start = rq->start;
+    a.rows.adapter = rq->adapter;
+    a.rows.requests = rq->count;
+    a.rows.ranks = ad->ranks;
+    a.rows.scale = ad->scale;
+    a.rows.count = ad->count;
+    a.rows.rank = ad->rank;
+    a.rows.T = T;
+    a.bf16 = ad->dtype == SFB_BF16;
+    a.row_adapter = reinterpret_cast<int32_t*>(ctx->ws);
+    return a;
+}
+
+// out = src times the shared matrix (transposed: by its columns) + H times the blocks' `out_factors`, where H, the projections of
+// src on `in_factors`, is made here too and left in `H` (H_out: and there).
 static int adapter_output(sfb_ctx* ctx, const AdapterLayout& l, const void* src, const void* W, const uint16_t* Wb, bool blocked,
-                          bool transposed, int64_t T, int64_t N, int64_t K, const sfb_adapters* ad, const void* factors, const float* H,
-                          void* out)
+                          bool transposed, int64_t T, int64_t N, int64_t K, const sfb_adapters* ad, const sfb_requests* rq,
+                          const void* in_factors, const void* out_factors, float* H, float* H_out, void* out)
 {
     const bool bf16 = ad->dtype == SFB_BF16;
     float* planes = reinterpret_cast<float*>(ctx->ws + l.off_planes);
+    sfb::AdapterProjectArgs a = project_args(ctx, T, ad, rq);
+    a.X = src;
+    a.F = in_factors;
+    a.K = K;
+    a.H = H;
+    a.H_out = H_out;
+    if (l.fused(bf16)) a.Hx = reinterpret_cast<uint16_t*>(ctx->ws + l.off_terms);
+    if (!l.few.dense) SFB_RUN(KID_ADAPTER_PROJECT, sfb::launch_adapter_project(a, ctx->dev, ctx->stream));
     sfb::AdapterJoinArgs j = {};
     j.planes = planes;
     j.split = l.split;
+    j.width = N;
     if (bf16) {
         sfb::AdapterBase b = {};
         b.A = static_cast<const uint16_t*>(src);
@@ -1108,15 +1137,19 @@ static int adapter_output(sfb_ctx* ctx, const AdapterLayout& l, const void* src,
         b.planes = planes;
         b.split = l.split;
         b.out = static_cast<uint16_t*>(out);
-        b.row_adapter = reinterpret_cast<const int32_t*>(ctx->ws);
-        b.Hx = reinterpret_cast<const uint16_t*>(ctx->ws + l.off_terms);
+        b.row_adapter = a.row_adapter;
+        b.Hx = a.Hx;
         b.H = H;
-        b.F = static_cast<const uint16_t*>(factors);
+        b.F = static_cast<const uint16_t*>(l.few.few ? in_factors : out_factors);
         b.ranks = ad->ranks;
         b.count = ad->count;
         b.rank = ad->rank;
-        SFB_RUN(KID_ADAPTER_BASE, sfb::launch_adapter_base_bf16(b, ctx->dev, ctx->stream));
-        if (l.split == 1) return SFB_OK;
+        if (l.few.few)
+            SFB_RUN(KID_ADAPTER_BASE, sfb::launch_adapter_few(b, l.few, a.rows, l.few.dense ? a.row_adapter : nullptr, ctx->dev, ctx->stream));
+        else
+            SFB_RUN(KID_ADAPTER_BASE, sfb::launch_adapter_base_bf16(b, ctx->dev, ctx->stream));
+        if (l.fused(bf16)) return SFB_OK;
+        if (l.few.few) j.width = l.few.width;
     } else {
         int parts = 1;
         sfb::GemmF32Args g = {};
@@ -1134,9 +1167,12 @@ static int adapter_output(sfb_ctx* ctx, const AdapterLayout& l, const void* src,
             j.split = parts;
         }
     }
-    j.row_adapter = reinterpret_cast<const int32_t*>(ctx->ws);
+    j.row_adapter = a.row_adapter;
+    j.dense = l.few.dense;
     j.H = H;
-    j.F = factors;
+    j.H_out = H_out;
+    j.scale = ad->scale;
+    j.F = out_factors;
     j.ranks = ad->ranks;
     j.count = ad->count;
     j.rank = ad->rank;
@@ -1146,22 +1182,6 @@ static int adapter_output(sfb_ctx* ctx, const AdapterLayout& l, const void* src,
     j.N = N;
     SFB_RUN(KID_ADAPTER_JOIN, sfb::launch_adapter_join(j, ctx->stream));
     return SFB_OK;
-}
-
-static sfb::AdapterProjectArgs project_args(sfb_ctx* ctx, int64_t T, const sfb_adapters* ad, const sfb_requests* rq)
-{
-    sfb::AdapterProjectArgs a = {};
-    a.rows.start = rq->start;
-    a.rows.adapter = rq->adapter;
-    a.rows.requests = rq->count;
-    a.rows.ranks = ad->ranks;
-    a.rows.scale = ad->scale;
-    a.rows.count = ad->count;
-    a.rows.rank = ad->rank;
-    a.rows.T = T;
-    a.bf16 = ad->dtype == SFB_BF16;
-    a.row_adapter = reinterpret_cast<int32_t*>(ctx->ws);
-    return a;
 }
 
 int sfb_adapter_forward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J, int64_t D, const void* X, int64_t T,
@@ -1178,15 +1198,7 @@ int sfb_adapter_forward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J,
     if (!ctx->ws || ctx->ws_bytes < l.total) return SFB_ENOWS;
     const DeviceScope scope(ctx->device);
     SFB_TRY(scope.status);
-    sfb::AdapterProjectArgs a = project_args(ctx, T, ad, rq);
-    a.X = X;
-    a.F = ad->V;
-    a.K = D;
-    a.H = reinterpret_cast<float*>(ctx->ws + l.off_h);
-    a.H_out = H;
-    if (a.bf16 && l.split == 1) a.Hx = reinterpret_cast<uint16_t*>(ctx->ws + l.off_terms);
-    SFB_RUN(KID_ADAPTER_PROJECT, sfb::launch_adapter_project(a, ctx->dev, ctx->stream));
-    return adapter_output(ctx, l, X, W, Wb, blocked, false, T, J, D, ad, ad->U, a.H, Y);
+    return adapter_output(ctx, l, X, W, Wb, blocked, false, T, J, D, ad, rq, ad->V, ad->U, reinterpret_cast<float*>(ctx->ws + l.off_h), H, Y);
 }
 
 int sfb_adapter_backward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J, int64_t D, const void* X, const void* dY, int64_t T,
@@ -1216,15 +1228,15 @@ int sfb_adapter_backward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J
         a.H = Hw;
         SFB_RUN(KID_ADAPTER_PROJECT, sfb::launch_adapter_project(a, ctx->dev, ctx->stream));
     }
-    a.X = dY;
-    a.F = ad->U;
-    a.K = J;
-    a.H = dH;
-    if (a.bf16 && l.split == 1) a.Hx = reinterpret_cast<uint16_t*>(ctx->ws + l.off_terms);
-    SFB_RUN(KID_ADAPTER_PROJECT, sfb::launch_adapter_project(a, ctx->dev, ctx->stream));
     if (dX && rows) {
-        rc = adapter_output(ctx, l, dY, W, Wb, blocked, true, T, D, J, ad, ad->V, dH, dX);
+        rc = adapter_output(ctx, l, dY, W, Wb, blocked, true, T, D, J, ad, rq, ad->U, ad->V, dH, nullptr, dX);
         if (rc != SFB_OK) return rc;
+    } else {
+        a.X = dY;
+        a.F = ad->U;
+        a.K = J;
+        a.H = dH;
+        SFB_RUN(KID_ADAPTER_PROJECT, sfb::launch_adapter_project(a, ctx->dev, ctx->stream));
     }
     if (!grads) return SFB_OK;
     sfb::AdapterOuterArgs o = {};

@@ -75,6 +75,8 @@ CASES = [
     (700, 128, 640, 40, 5, 200, False, 0, 0),
     (1100, 520, 264, 1, 12, 1, False, 0, 0),
     (2600, 264, 520, 2, 40, 7, False, 5, 9),
+    (12, 1032, 1032, 40, 256, 7, False, 0, 0),
+    (128, 2056, 1536, 9, 33, 100, False, 2, 1),
 ]
 
 
