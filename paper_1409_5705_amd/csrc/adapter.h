@@ -64,10 +64,10 @@ int adapter_base_split(int64_t M, int64_t N, int64_t K);
 
 // The same for few rows: planes alone, of `width` columns; with `dense` those behind the N of the product are A times the
 // factors of all blocks ([count][rank][K]).  row_adapter (nullable): written as launch_adapter_project does.
-constexpr int64_t FEW_ROWS = 128;
+constexpr int64_t FEW_ROWS = 256;
 struct AdapterFewPlan {
     bool few = false, dense = false;
-    int split = 1;
+    int split = 1, tile_m = 64;
     int64_t width = 0;
 };
 AdapterFewPlan adapter_few_plan(int64_t M, int64_t N, int64_t K, int64_t factors);

@@ -16,7 +16,7 @@ struct DeviceInfo {
     bool apply_gather_lds_set[2] = {};                   // of the apply of sparse factors (fp32 array, planes)
     bool fwd_stream_lds_set[6] = {};                     // and of the streaming bf16 forward
     bool adapter_base_lds_set[8] = {};                   // and of the product beside the factor blocks (tile, orientation, split)
-    bool adapter_few_lds_set[2] = {};                    // (its form for few rows: orientation)
+    bool adapter_few_lds_set[4] = {};                    // (its form for few rows: rows of a tile, orientation)
     int softmax_wait_polls = 1000;                 // bound of the one-read softmax's wait for a partner's word
 };
 

@@ -504,8 +504,8 @@ hipError_t launch_base(BaseParams& p, DeviceInfo& dev, hipStream_t stream)
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------------------
-// The stream of W bounds the product of up to FEW_ROWS rows.  Tiles of 64 x 64 along a part of k, five LDS stages of a k-slice
-// each: 128 KB of requests of a CU's two workgroups in flight.  The blocks' factors are taken for further columns of the matrix:
+// The stream of W bounds the product of up to FEW_ROWS rows.  Tiles of 64 or 128 rows x 64 columns along a part of k, five or
+// three LDS stages of a k-slice: about 100 KB of requests of a CU's two workgroups in flight.  The blocks' factors are taken for further columns of the matrix:
 // every row is multiplied with the factors of all blocks (the matrix pipes have the time), and the join picks its own block's.
 struct FewParams {
     const uint16_t* A;
@@ -517,12 +517,14 @@ struct FewParams {
     AdapterRows rows;
     int32_t* row_adapter;      // nullable: written by the last workgroup
 };
-constexpr int NS = 5;
+constexpr int few_stages(int fm) { return fm == 2 ? 5 : 3; }
 
-template <bool TRANSPOSED>
+// FM: 32 FM rows; 2 x 2 wavefronts of 16 FM x 32.
+template <bool TRANSPOSED, int FM>
 __global__ __launch_bounds__(256) void adapter_few_kernel(FewParams p)
 {
-    constexpr uint32_t TILE = 64 * 128, STAGE_BYTES = 2 * TILE;
+    constexpr int NS = few_stages(FM);
+    constexpr uint32_t A_BYTES = 32 * FM * 128, STAGE_BYTES = A_BYTES + 64 * 128;
     extern __shared__ u32x4 smem[];
     char* const lds = reinterpret_cast<char*>(smem);
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
@@ -541,8 +543,8 @@ __global__ __launch_bounds__(256) void adapter_few_kernel(FewParams p)
         }
         return;
     }
-    const int wm0 = (wave >> 1) * 32, wn0 = (wave & 1) * 32;
-    const int64_t m0 = (int64_t)(blockIdx.x % (unsigned)p.tiles_m) * 64;
+    const int wm0 = (wave >> 1) * 16 * FM, wn0 = (wave & 1) * 32;
+    const int64_t m0 = (int64_t)(blockIdx.x % (unsigned)p.tiles_m) * (32 * FM);
     const int tile = (int)(blockIdx.x / (unsigned)p.tiles_m);
     const bool factor = tile >= p.tiles_w;                 // columns of the blocks' factors, k-contiguous
     const bool transposed = TRANSPOSED && !factor;
@@ -553,14 +555,18 @@ __global__ __launch_bounds__(256) void adapter_few_kernel(FewParams p)
     const int s_begin = (int)((int64_t)slices * blockIdx.y / p.split), nk = (int)((int64_t)slices * (blockIdx.y + 1) / p.split) - s_begin;
 
     const uint32_t lda = (uint32_t)p.K * 2u, ldw = pitch ? (uint32_t)BK * 2u : (uint32_t)ldw_e * 2u;
-    const int last_m = (int)(p.M - m0 < 64 ? p.M - m0 : 64), last_n = (int)(N - n0 < 64 ? N - n0 : 64);
-    uint32_t offA[2], offB[2];
-    int kA[2], kB[2];                                      // first k of what a lane loads
+    const int last_m = (int)(p.M - m0 < 32 * FM ? p.M - m0 : 32 * FM), last_n = (int)(N - n0 < 64 ? N - n0 : 64);
+    uint32_t offA[FM], offB[2];
+    int kA[FM], kB[2];                                     // first k of what a lane loads
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int r = 8 * (FM * wave + i) + (lane >> 3), c = (lane & 7) ^ swz(r);
+        offA[i] = r < last_m ? (uint32_t)r * lda + (uint32_t)c * 16u : OUT_OF_RANGE;
+        kA[i] = 8 * c;
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int r = 8 * (2 * wave + i) + (lane >> 3), c = (lane & 7) ^ swz(r);
-        offA[i] = r < last_m ? (uint32_t)r * lda + (uint32_t)c * 16u : OUT_OF_RANGE;
-        kA[i] = 8 * c;
         if (transposed) {
             const int u = (lane & 7) ^ ((r & 1) << 2);     // LDS rows of 64 columns; chunk u of row r in slot u ^ 4 (r % 2)
             offB[i] = 8 * u < last_n ? (uint32_t)r * ldw + (uint32_t)u * 16u : OUT_OF_RANGE;
@@ -578,35 +584,39 @@ __global__ __launch_bounds__(256) void adapter_few_kernel(FewParams p)
                                        : (pitch ? (uint64_t)(((n0 / BM) * (pitch / BK) + k0 / BK) * (BM * BK) + (n0 % BM) * BK) : (uint64_t)(n0 * ldw_e + k0));
         const u32x4 ra = descriptor(reinterpret_cast<uint64_t>(p.A) + (uint64_t)(m0 * p.K + k0) * 2u);
         const u32x4 rb = descriptor(reinterpret_cast<uint64_t>(W) + at * 2u);
-        const uint32_t dst = lds_base + (uint32_t)(s % NS) * STAGE_BYTES + (uint32_t)wave * 2048u;
-        buffer_to_lds_16<0>(dst, ra, kA[0] < left ? offA[0] : OUT_OF_RANGE);
-        buffer_to_lds_16<1024>(dst, ra, kA[1] < left ? offA[1] : OUT_OF_RANGE);
-        buffer_to_lds_16<TILE>(dst, rb, kB[0] < left ? offB[0] : OUT_OF_RANGE);
-        buffer_to_lds_16<TILE + 1024>(dst, rb, kB[1] < left ? offB[1] : OUT_OF_RANGE);
+        const uint32_t stage = lds_base + (uint32_t)(s % NS) * STAGE_BYTES;
+        static_for<0, FM>([&](auto I) {
+            constexpr int i = decltype(I)::value;
+            buffer_to_lds_16<i * 1024u>(stage + (uint32_t)(FM * wave) * 1024u, ra, kA[i] < left ? offA[i] : OUT_OF_RANGE);
+        });
+        static_for<0, 2>([&](auto I) {
+            constexpr int i = decltype(I)::value;
+            buffer_to_lds_16<A_BYTES + i * 1024u>(stage + (uint32_t)(2 * wave) * 1024u, rb, kB[i] < left ? offB[i] : OUT_OF_RANGE);
+        });
     };
-    floatx4 acc[2][2];
+    floatx4 acc[FM][2];
 #pragma unroll
-    for (int ta = 0; ta < 2; ++ta)
+    for (int ta = 0; ta < FM; ++ta)
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) acc[ta][tb] = floatx4{0.f, 0.f, 0.f, 0.f};
     for (int s = 0; s < NS - 1; ++s) issue(s);
     for (int s = 0; s < nk; ++s) {
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * (NS - 2)) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((FM + 2) * (NS - 2)) : "memory");
         __syncthreads();                                   // slice s is in LDS; every wavefront has read the slice before
         issue(s + NS - 1);
         const char* const stage = lds + (uint32_t)(s % NS) * STAGE_BYTES;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-            bf16x8 a[2], b[2];
+            bf16x8 a[FM], b[2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            for (int t = 0; t < FM; ++t) {
                 const int r = wm0 + 16 * t + l16;
                 a[t] = *reinterpret_cast<const bf16x8*>(stage + r * 128 + (((4 * ks + quad) ^ swz(r)) << 4));
             }
             if (transposed) {
                 // lane i of a group: row i / 4 of four, piece i % 4 of the 32 columns of the wavefront
                 const int r = 32 * ks + 8 * quad + (l16 >> 2);
-                const char* const at = stage + TILE + r * 128 + ((((wn0 >> 3) + (l16 & 3)) ^ ((r & 1) << 2)) << 4);
+                const char* const at = stage + A_BYTES + r * 128 + ((((wn0 >> 3) + (l16 & 3)) ^ ((r & 1) << 2)) << 4);
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * t));
@@ -617,17 +627,17 @@ __global__ __launch_bounds__(256) void adapter_few_kernel(FewParams p)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const int r = wn0 + 16 * t + l16;
-                    b[t] = *reinterpret_cast<const bf16x8*>(stage + TILE + r * 128 + (((4 * ks + quad) ^ swz(r)) << 4));
+                    b[t] = *reinterpret_cast<const bf16x8*>(stage + A_BYTES + r * 128 + (((4 * ks + quad) ^ swz(r)) << 4));
                 }
             }
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-                for (int ta = 0; ta < 2; ++ta) acc[ta][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[tb], a[ta], acc[ta][tb], 0, 0, 0);
+                for (int ta = 0; ta < FM; ++ta) acc[ta][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[tb], a[ta], acc[ta][tb], 0, 0, 0);
         }
     }
 #pragma unroll
-    for (int ta = 0; ta < 2; ++ta) {
+    for (int ta = 0; ta < FM; ++ta) {
         const int64_t m = m0 + wm0 + 16 * ta + l16;
         if (m >= p.M) continue;
         float* const row = p.planes + ((int64_t)blockIdx.y * p.M + m) * p.width + (factor ? p.N : 0) + n0 + wn0;
@@ -638,6 +648,20 @@ __global__ __launch_bounds__(256) void adapter_few_kernel(FewParams p)
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+template <bool TRANSPOSED, int FM>
+hipError_t launch_few(const FewParams& p, dim3 grid, DeviceInfo& dev, hipStream_t stream)
+{
+    constexpr int lds = few_stages(FM) * (32 * FM + 64) * 128;
+    bool& set = dev.adapter_few_lds_set[(TRANSPOSED ? 1 : 0) + (FM == 2 ? 0 : 2)];
+    if (!set) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&adapter_few_kernel<TRANSPOSED, FM>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+        set = true;
+    }
+    adapter_few_kernel<TRANSPOSED, FM><<<grid, 256, lds, stream>>>(p);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -659,9 +683,18 @@ AdapterFewPlan adapter_few_plan(int64_t M, int64_t N, int64_t K, int64_t factors
     // the factors of the whole pool, or a launch of its own for those that are used: it takes as long as 16 MB of them
     f.dense = factors * K <= (8 << 20);
     f.width = N + (f.dense ? (factors + 3) / 4 * 4 : 0);
-    const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64 + (f.dense ? (factors + 63) / 64 : 0)), slices = (K + BK - 1) / BK;
-    const int64_t s = std::min(512 / tiles, slices / 6);
-    f.split = s < 1 ? 1 : s > 16 ? 16 : (int)s;
+    f.tile_m = M <= 64 ? 64 : 128;
+    // The parts of k: rounds of 512 workgroups of so many slices, 0.5 us each, and 3 us around them; planes that are written and
+    // read at 4 TB/s.
+    const int64_t tiles = ((M + f.tile_m - 1) / f.tile_m) * ((N + 63) / 64 + (f.dense ? (factors + 63) / 64 : 0)), slices = (K + BK - 1) / BK;
+    double best = 0;
+    for (int s = 1; s <= 16 && (s == 1 || slices / s >= 4); ++s) {
+        const double us = (double)((tiles * s + 511) / 512) * (0.5 * (double)((slices + s - 1) / s) + 3.0) + (double)(s * M * f.width) * 8e-6 / 4.0;
+        if (s == 1 || us < best) {
+            best = us;
+            f.split = s;
+        }
+    }
     return f;
 }
 
@@ -679,24 +712,13 @@ hipError_t launch_adapter_few(const AdapterBase& a, const AdapterFewPlan& plan, 
     p.width = plan.width;
     p.planes = a.planes;
     p.split = plan.split;
-    p.tiles_m = (int)((a.M + 63) / 64);
+    p.tiles_m = (int)((a.M + plan.tile_m - 1) / plan.tile_m);
     p.tiles_w = (int)((a.N + 63) / 64);
     p.rows = rows;
     p.row_adapter = row_adapter;
-    constexpr int lds = NS * 2 * 64 * 128;
-    const void* const kernel = a.transposed ? reinterpret_cast<const void*>(&adapter_few_kernel<true>) : reinterpret_cast<const void*>(&adapter_few_kernel<false>);
-    bool& set = dev.adapter_few_lds_set[a.transposed ? 1 : 0];
-    if (!set) {
-        const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        if (e != hipSuccess) return e;
-        set = true;
-    }
     const dim3 grid((unsigned)(p.tiles_m * (p.tiles_w + (p.factors + 63) / 64) + (row_adapter ? 1 : 0)), (unsigned)plan.split);
-    if (a.transposed)
-        adapter_few_kernel<true><<<grid, 256, lds, stream>>>(p);
-    else
-        adapter_few_kernel<false><<<grid, 256, lds, stream>>>(p);
-    return hipGetLastError();
+    if (plan.tile_m == 64) return a.transposed ? launch_few<true, 2>(p, grid, dev, stream) : launch_few<false, 2>(p, grid, dev, stream);
+    return a.transposed ? launch_few<true, 4>(p, grid, dev, stream) : launch_few<false, 4>(p, grid, dev, stream);
 }
 
 hipError_t launch_adapter_base_bf16(const AdapterBase& a, DeviceInfo& dev, hipStream_t stream)

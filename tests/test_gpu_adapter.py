@@ -77,6 +77,7 @@ CASES = [
     (2600, 264, 520, 2, 40, 7, False, 5, 9),
     (12, 1032, 1032, 40, 256, 7, False, 0, 0),
     (128, 2056, 1536, 9, 33, 100, False, 2, 1),
+    (256, 2056, 1544, 9, 33, 12, False, 0, 1),
 ]
 
 
