@@ -283,69 +283,78 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
             left[i] = __builtin_amdgcn_ballot_w64(block[i] >= 0 && block[i] < p.count);
         }
         const int pitch = adapter_pitch(p.rank);
-        // a chunk's H of all the wavefront's rows, loaded together and a chunk ahead (what rows of other blocks hold is not used)
+        // the H of 16 pairs of all the wavefront's rows (what rows of other blocks hold is not used)
         const uint16_t* hx[TM];
 #pragma unroll
         for (int ta = 0; ta < TM; ++ta) {
             const int64_t m = m0 + wm0 + 16 * ta + l16;
             hx[ta] = p.Hx + (m < p.M ? m : p.M - 1) * (2 * pitch) + 8 * quad;
         }
-        u32x4 ahead[TM];
-        auto load_h = [&](int r0) {
+        u32x4 h[TM];
+        int h_from = -1;
+        // Rounds of four chunks of 16 pairs, the first 16 of all blocks and then the next: LDS rows of TBN columns as W's, transposed.
+        // Lane k knows the k-th chunk's block, first pair and the block's rank.
+        uint64_t all[TBM / 64];
 #pragma unroll
-            for (int ta = 0; ta < TM; ++ta) ahead[ta] = *reinterpret_cast<const u32x4*>(hx[ta] + 2 * r0);
-        };
-        // Rounds of four chunks of 16 pairs, of whatever blocks: LDS rows of TBN columns as W's, transposed.
-        int cur = -1, cur_r = 0, cur_rank = 0;
+        for (int i = 0; i < TBM / 64; ++i) all[i] = left[i];
+        int cur_r = 0;
         for (;;) {
-            int of[4], from[4], ranks[4];          // block, first pair, the block's rank
+            int of = -1, from = 0, ranks = 0, chunks = 0;
+            while (chunks < 4 && cur_r < p.rank) {
+                int a = -1;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (cur_r >= cur_rank) {
-                    cur = -1;
+                for (int i = 0; i < TBM / 64; ++i)
+                    if (a < 0 && left[i]) a = __builtin_amdgcn_readlane(block[i], (int)__builtin_ctzll(left[i]));
+                if (a < 0) {                       // the next 16
+                    cur_r += 16;
 #pragma unroll
-                    for (int i = 0; i < TBM / 64; ++i)
-                        if (cur < 0 && left[i]) cur = __builtin_amdgcn_readlane(block[i], (int)__builtin_ctzll(left[i]));
-                    cur_r = 0;
-                    cur_rank = cur < 0 ? 0 : __builtin_amdgcn_readfirstlane(rank_of(p.ranks, p.rank, cur));
-#pragma unroll
-                    for (int i = 0; i < TBM / 64; ++i) left[i] &= ~__builtin_amdgcn_ballot_w64(block[i] == cur);
+                    for (int i = 0; i < TBM / 64; ++i) left[i] = all[i];
+                    continue;
                 }
-                of[k] = cur;
-                from[k] = cur_r;
-                ranks[k] = cur_rank;
-                cur_r += 16;
-            }
-            if (of[0] < 0) break;
-            __syncthreads();                       // (the chunks before have been read)
+                const int rank = __builtin_amdgcn_readfirstlane(rank_of(p.ranks, p.rank, a));
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (of[k] < 0) continue;
-                const uint64_t factors = reinterpret_cast<uint64_t>(p.F) + (uint64_t)(((int64_t)of[k] * p.rank + from[k]) * p.N + n0) * 2u;
+                for (int i = 0; i < TBM / 64; ++i) {
+                    const uint64_t its = __builtin_amdgcn_ballot_w64(block[i] == a);
+                    left[i] &= ~its;
+                    if (rank <= cur_r + 16) all[i] &= ~its;
+                }
+                if (cur_r >= rank) continue;
+                if (lane == chunks) {
+                    of = a;
+                    from = cur_r;
+                    ranks = rank;
+                }
+                ++chunks;
+            }
+            if (chunks == 0) break;
+            __syncthreads();                       // (the chunks before have been read)
+            for (int k = 0; k < chunks; ++k) {
+                const int a = __builtin_amdgcn_readlane(of, k), r0 = __builtin_amdgcn_readlane(from, k), rank = __builtin_amdgcn_readlane(ranks, k);
+                const uint64_t factors = reinterpret_cast<uint64_t>(p.F) + (uint64_t)(((int64_t)a * p.rank + r0) * p.N + n0) * 2u;
                 static_for<0, (int)(F_CHUNK / 4096)>([&](auto I) {
                     constexpr int PER = (int)(F_CHUNK / 4096);
                     const int r = (PER * wave + decltype(I)::value) * RPL + lane / SLOTS, u = (lane % SLOTS) ^ ((r & 3) << 2);
-                    const bool in = from[k] + r < ranks[k] && n0 + 8 * u < p.N;
-                    buffer_to_lds_16<F_OFF + decltype(I)::value * 1024u>(lds_base + (uint32_t)k * F_CHUNK + (uint32_t)(PER * wave) * 1024u, descriptor(factors),
-                                                                       in ? (uint32_t)r * (uint32_t)(p.N * 2) + (uint32_t)u * 16u : OUT_OF_RANGE);
+                    const bool in = r0 + r < rank && n0 + 8 * u < p.N;
+                    buffer_to_lds_16<decltype(I)::value * 1024u>(lds_base + F_OFF + (uint32_t)k * F_CHUNK + (uint32_t)(PER * wave) * 1024u, descriptor(factors),
+                                                               in ? (uint32_t)r * (uint32_t)(p.N * 2) + (uint32_t)u * 16u : OUT_OF_RANGE);
                 });
             }
-            load_h(from[0]);
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
             {
 #pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    const int a = c == 0 ? of[0] : c == 1 ? of[1] : c == 2 ? of[2] : of[3];
-                    if (a < 0) break;
-                    u32x4 h[TM];
+                for (int c = 0; c < chunks; ++c) {
+                    const int a = __builtin_amdgcn_readlane(of, c);
+                    const int r0 = __builtin_amdgcn_readlane(from, c);
+                    if (r0 != h_from) {
+                        h_from = r0;
 #pragma unroll
-                    for (int ta = 0; ta < TM; ++ta) {
-                        h[ta] = u32x4{0u, 0u, 0u, 0u};
-                        if (mine[ta] == a) h[ta] = ahead[ta];
+                        for (int ta = 0; ta < TM; ++ta) h[ta] = *reinterpret_cast<const u32x4*>(hx[ta] + 2 * r0);
                     }
-                    const int next = c == 0 ? 1 : c == 1 ? 2 : 3;
-                    if (c < 3 && (next == 1 ? of[1] : next == 2 ? of[2] : of[3]) >= 0) load_h(next == 1 ? from[1] : next == 2 ? from[2] : from[3]);
+                    bool used = false;
+#pragma unroll
+                    for (int ta = 0; ta < TM; ++ta) used = used || __builtin_amdgcn_ballot_w64(mine[ta] == a) != 0;
+                    if (!used) continue;
                     u32x4 f[TN];
                     uint32_t least = 0x7f807f80u;      // of both halves; 0: not finite
 #pragma unroll
@@ -378,9 +387,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
 #pragma unroll
                     for (int ta = 0; ta < TM; ++ta) {
                         if (__builtin_amdgcn_ballot_w64(mine[ta] == a) == 0) continue;
+                        u32x4 ha = {0u, 0u, 0u, 0u};
+                        if (mine[ta] == a) ha = h[ta];
 #pragma unroll
                         for (int tb = 0; tb < TN; ++tb)
-                            acc[ta][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f[tb]), __builtin_bit_cast(bf16x8, h[ta]), acc[ta][tb], 0, 0, 0);
+                            acc[ta][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f[tb]), __builtin_bit_cast(bf16x8, ha), acc[ta][tb], 0, 0, 0);
                     }
                 }
             }
@@ -508,7 +519,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
                 mine[ta] = m < p.M ? p.row_adapter[m] : ROW_OUTSIDE;
             }
             special = blocks_part(m0, n0);
+            // (vmcnt(0): a load that nobody has waited for, one of H, would have the compiler wait in every slice)
+            __builtin_amdgcn_s_waitcnt(0x0f70);
         }
+#pragma unroll
+        for (int ta = 0; ta < TM; ++ta)
+#pragma unroll
+            for (int tb = 0; tb < TN; ++tb) asm volatile("" : "+a"(acc[ta][tb]));
         for (int k = 0; k < nk; ++k) slice_body();
         epilogue(m0, n0);
         if (!SPLIT && special) add_special(m0, n0);
