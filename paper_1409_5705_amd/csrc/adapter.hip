@@ -56,37 +56,10 @@ __device__ __forceinline__ floatx4 mfma_chunk(u32x4 a, u32x4 b, floatx4 acc)
     }
 }
 
-struct ProjectParams {
-    AdapterRows rows;
-    const void* X;
-    const void* F;
-    int64_t K;
-    int32_t* row_adapter;
-    float* H;
-    float* H_out;
-    uint16_t* Hx;
-    int pitch;
-};
-
-// Two bf16 terms of a value: its upper half and what is left, rounded (together off by at most 2^-17 of the value, and of its
-// sign); one that is not finite as itself twice.
-__device__ __forceinline__ void two_terms(float v, uint16_t& first, uint16_t& second)
-{
-    const uint32_t bits = __float_as_uint(v);
-    const bool finite = (~bits & 0x7f800000u) != 0;
-    first = (uint16_t)(finite ? bits >> 16 : pack_bf16(v, 0.f));
-    second = (uint16_t)pack_bf16(finite ? v - __uint_as_float(bits & 0xffff0000u) : v, 0.f);
-}
-// Place of pair r's first term in a row of the two-term array; the second one is 16 further.
-__device__ __forceinline__ int term_at(int r) { return (r >> 4) * 32 + (r & 15); }
-
 constexpr int64_t MAX_BLOCKS = 1 << 22;      // workgroups of a launch (threads of a grid are counted in 32 bits)
 
-// Up to 16 rows of one request against the 16 RT factors 16 RT * blockIdx.y ..; the wavefronts share k.  Workgroup w < windows
-// takes the rows from 16 w on, workgroup windows + q those from the first row of request q on, both to the next multiple of 16
-// or to the end of their request: every row once, and never two blocks in a workgroup.  (Tiles of 32 rows whatever the requests,
-// gone through once for every block in them: 8192 rows in 24 requests, K = 4096, 64 pairs 62 us.)
-// What bounds it is the stream of X: a wavefront's loads of U k-steps are in flight together.
+// Up to 16 rows of one request against the 16 RT factors 16 RT * blockIdx.y ..; the wavefronts share k.  For few tiles and fp32:
+// what bounds it is how soon everything is on its way, and a wavefront's loads of U k-steps are in flight together.
 template <typename T, int RT, int PW>
 __global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams p, unsigned windows, unsigned xcds)
 {
@@ -96,46 +69,10 @@ __global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams 
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r0 = (int)blockIdx.y * 16 * RT;
     const AdapterRows& rows = p.rows;
-    int64_t t0, q;
-    // neighbours, which are likely to use the same factors, go to the same XCD
-    unsigned tile = blockIdx.x;
-    {
-        const unsigned first = tile < windows ? 0 : windows, count = first ? gridDim.x - windows : windows;
-        const unsigned whole = count / xcds * xcds, i = tile - first;
-        if (i < whole) tile = first + i % xcds * (whole / xcds) + i / xcds;
-    }
-    if (tile < windows) {
-        t0 = (int64_t)tile * 16;
-        const int64_t t = t0 + tid;
-        if (tid < 16 && blockIdx.y == 0 && t < rows.T && (t < rows.start[0] || t >= rows.start[rows.requests])) p.row_adapter[t] = ROW_OUTSIDE;
-        q = request_of(rows.start, rows.requests, t0, lane);
-        if (q < 0) return;
-    } else {
-        q = tile - windows;
-        t0 = rows.start[q];
-        if (t0 < 0 || t0 >= rows.T || (t0 & 15) == 0) return;
-    }
-    int64_t t1 = (t0 | 15) + 1;
-    if (rows.start[q + 1] < t1) t1 = rows.start[q + 1];
-    if (rows.T < t1) t1 = rows.T;
-    const int n_rows = (int)(t1 - t0);
-    if (n_rows <= 0) return;
-    int a = rows.adapter[q];
-    const int rank = a < 0 || a >= rows.count ? 0 : rank_of(rows.ranks, rows.rank, a);
-    if (rank == 0) a = ROW_NONE;
-    if (blockIdx.y == 0 && tid < n_rows) p.row_adapter[t0 + tid] = a;
-    if (r0 >= rank) {      // no factors here: zeros
-        for (int i = tid; i < n_rows * 16 * RT; i += 64 * PW) {
-            const int64_t t = t0 + i / (16 * RT);
-            const int r = r0 + i % (16 * RT);
-            if (r < p.pitch) {
-                p.H[t * p.pitch + r] = 0.f;
-                if (p.Hx) p.Hx[t * 2 * p.pitch + term_at(r)] = p.Hx[t * 2 * p.pitch + term_at(r) + 16] = 0;
-            }
-            if (p.H_out && r < rows.rank) p.H_out[t * rows.rank + r] = 0.f;
-        }
-        return;
-    }
+    ProjectTile tile;
+    if (!project_tile<16>(p, windows, xcds, r0, 16 * RT, tid, 64 * PW, lane, tile)) return;
+    const int64_t t0 = tile.t0;
+    const int n_rows = tile.rows, rank = tile.rank, a = tile.a;
 
     const int64_t steps = (p.K + STEP - 1) / STEP, per = (steps + PW - 1) / PW;
     const int64_t k_begin = wave * per * STEP, k_end = k_begin + per * STEP < p.K ? k_begin + per * STEP : p.K;
@@ -176,28 +113,7 @@ __global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams 
     floatx4 sum = part[0][wave][lane];
 #pragma unroll
     for (int w = 1; w < PW; ++w) sum += part[w][wave][lane];
-    if (l16 >= n_rows) return;
-    const float s = rows.scale ? rows.scale[a] : 1.f;
-    const int64_t t = t0 + l16;
-    const int r = r0 + 16 * wave + 4 * quad;
-    if (r >= p.pitch) return;
-    float h[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) h[e] = r + e < rank ? s * sum[e] : 0.f;
-    *reinterpret_cast<floatx4*>(p.H + t * p.pitch + r) = floatx4{h[0], h[1], h[2], h[3]};
-    if (p.Hx) {
-        uint16_t first[4], second[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) two_terms(h[e], first[e], second[e]);
-        uint16_t* const at = p.Hx + t * 2 * p.pitch + term_at(r);
-        *reinterpret_cast<u32x2*>(at) = u32x2{(uint32_t)first[0] | (uint32_t)first[1] << 16, (uint32_t)first[2] | (uint32_t)first[3] << 16};
-        *reinterpret_cast<u32x2*>(at + 16) = u32x2{(uint32_t)second[0] | (uint32_t)second[1] << 16, (uint32_t)second[2] | (uint32_t)second[3] << 16};
-    }
-    if (p.H_out) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (r + e < rows.rank) p.H_out[t * rows.rank + r + e] = h[e];
-    }
+    store_projection(p, tile, t0 + l16, l16 < n_rows, r0 + 16 * wave + 4 * quad, sum);
 }
 
 // A thread: four columns of one row of the output.  The row's projections come from H, or (dense) from the planes, which hold
@@ -424,7 +340,7 @@ void project_start(const ProjectParams& p, dim3 grid, unsigned windows, const De
 {
     const unsigned xcds = dev.xcds > 0 ? dev.xcds : 1;
     // few workgroups: 16 wavefronts share k, and all of a row is on its way at once; many: eight, and two or three workgroups a
-    // CU hide each other's start (8192 rows, K = 4096, 16 pairs: 30 us with 16, 27 with 8)
+    // CU hide each other's start (8192 rows, K = 4096, 16 pairs: 30 and 27 us)
     if ((int64_t)grid.x * grid.y < dev.cus)
         adapter_project_kernel<T, RT, 16><<<grid, 64 * 16, 0, stream>>>(p, windows, xcds);
     else
@@ -475,6 +391,9 @@ hipError_t launch_adapter_project(const AdapterProjectArgs& a, DeviceInfo& dev, 
 {
     if (a.rows.T <= 0) return hipSuccess;
     ProjectParams p = {a.rows, a.X, a.F, a.K, a.row_adapter, a.H, a.H_out, a.Hx, adapter_pitch(a.rows.rank)};
+    // whole tiles of 32 rows where there are as many as half of the CUs, and rows enough of a request to fill them
+    if (a.bf16 && p.pitch > 0 && a.rows.T >= 16 * (int64_t)dev.cus && a.rows.T >= 16 * a.rows.requests && (a.rows.T + 31) / 32 + a.rows.requests <= MAX_BLOCKS)
+        return launch_adapter_project_tiles(p, dev, stream);
     return a.bf16 ? project_rank<uint16_t>(p, dev, stream) : project_rank<float>(p, dev, stream);
 }
 

@@ -553,6 +553,85 @@ hipError_t launch_base(BaseParams& p, DeviceInfo& dev, hipStream_t stream)
     return hipGetLastError();
 }
 
+// ---- projections of many rows ---------------------------------------------------------------------------------------------
+// H[t][r] = scale_a sum_k X[t][k] F_a[r][k] on tiles of 32 rows of one request (as adapter_project_kernel divides them) x 16 RT
+// factors.  The stream of X and the factors' way out of the L2 bound it: whole lines straight into LDS, six stages ahead.  (A
+// MFMA operand loaded from memory into its registers takes a line for every lane: 8192 rows, K = 4096, 64 pairs 61 us.)
+// Wavefront w: the k-step w % 2 of every 64 k and the rows 16 (w / 2) .. of the tile.
+template <int RT>
+__global__ __launch_bounds__(256) void adapter_project_tiles_kernel(ProjectParams p, unsigned windows, unsigned xcds)
+{
+    constexpr int KM = RT == 1 ? 2 : 1, PS = 6, LOADS = KM * (4 + 2 * RT) / 4;      // 64 KM of k a slice; loads of a wavefront
+    static_assert(KM * (4 + 2 * RT) % 4 == 0, "as many loads for every wavefront");
+    constexpr uint32_t ROWS_BYTES = 32 * 128, SLAB = ROWS_BYTES + 16 * RT * 128, STAGE_BYTES = KM * SLAB;
+    __shared__ u32x4 smem[PS * STAGE_BYTES / 16];
+    const char* const lds = reinterpret_cast<const char*>(smem);
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    ProjectTile tile;
+    if (!project_tile<32>(p, windows, xcds, 16 * RT * (int)blockIdx.y, 16 * RT, tid, 256, lane, tile)) return;
+    const int r0 = 16 * RT * (int)blockIdx.y;
+
+    // load j of a slice: 8 rows of slab j / (4 + 2 RT), of X or of the factors
+    uint32_t off[LOADS], to[LOADS];
+    int k_of[LOADS];
+    bool is_x[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int j = LOADS * wave + i, slab = j / (4 + 2 * RT), b = j % (4 + 2 * RT);
+        is_x[i] = b < 4;
+        const int r = 8 * (is_x[i] ? b : b - 4) + (lane >> 3), c = (lane & 7) ^ swz(r);
+        k_of[i] = 64 * slab + 8 * c;
+        const bool in = is_x[i] ? r < tile.rows : r0 + r < tile.rank;
+        off[i] = in ? (uint32_t)r * (uint32_t)(p.K * 2) + (uint32_t)k_of[i] * 2u : OUT_OF_RANGE;
+        to[i] = (uint32_t)slab * SLAB + (is_x[i] ? 0u : ROWS_BYTES) + (uint32_t)(is_x[i] ? b : b - 4) * 1024u;
+    }
+    const uint64_t gx = uniform64(reinterpret_cast<uint64_t>(p.X) + (uint64_t)(tile.t0 * p.K) * 2u);
+    const uint64_t gf = uniform64(reinterpret_cast<uint64_t>(p.F) + (uint64_t)(((int64_t)tile.a * p.rows.rank + r0) * p.K) * 2u);
+    const int slices = (int)((p.K + 64 * KM - 1) / (64 * KM));
+    auto issue = [&](int s) {      // (past the last slice: nothing is in range)
+        const int64_t k0 = (int64_t)s * (64 * KM), left = p.K - k0;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            buffer_to_lds_16<0>(lds_base + (uint32_t)(s % PS) * STAGE_BYTES + to[i], descriptor((is_x[i] ? gx : gf) + (uint64_t)k0 * 2u),
+                                k_of[i] < left ? off[i] : OUT_OF_RANGE);
+    };
+    floatx4 acc[RT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    const int ks = wave & 1, row = 16 * (wave >> 1) + l16;
+    for (int s = 0; s < PS - 1; ++s) issue(s);
+    for (int s = 0; s < slices; ++s) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS * (PS - 2)) : "memory");
+        __syncthreads();                                   // slice s is in LDS; every wavefront has read the slice before
+        issue(s + PS - 1);
+        const char* const stage = lds + (uint32_t)(s % PS) * STAGE_BYTES;
+#pragma unroll
+        for (int m = 0; m < KM; ++m) {
+            const bf16x8 x = *reinterpret_cast<const bf16x8*>(stage + m * SLAB + row * 128 + (((4 * ks + quad) ^ swz(row)) << 4));
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                const int r = 16 * i + l16;
+                const bf16x8 f = *reinterpret_cast<const bf16x8*>(stage + m * SLAB + ROWS_BYTES + r * 128 + (((4 * ks + quad) ^ swz(r)) << 4));
+                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, x, acc[i], 0, 0, 0);
+            }
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    floatx4* const part = reinterpret_cast<floatx4*>(smem);      // the odd k-steps' sums
+    if (ks == 1) {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) part[((wave >> 1) * RT + i) * 64 + lane] = acc[i];
+    }
+    __syncthreads();
+    if (ks == 1) return;
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+        store_projection(p, tile, tile.t0 + row, row < tile.rows, r0 + 16 * i + 4 * quad, acc[i] + part[((wave >> 1) * RT + i) * 64 + lane]);
+}
+
 // ---- few rows ------------------------------------------------------------------------------------------------------------
 // The stream of W bounds the product of up to FEW_ROWS rows.  Tiles of 64 or 128 rows x 64 columns along a part of k, five or
 // three LDS stages of a k-slice: about 100 KB of requests of a CU's two workgroups in flight.  The blocks' factors are taken for further columns of the matrix:
@@ -700,6 +779,15 @@ __global__ __launch_bounds__(256) void adapter_few_kernel(FewParams p)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
+template <int RT>
+hipError_t launch_project_tiles(const ProjectParams& p, DeviceInfo& dev, hipStream_t stream)
+{
+    const int64_t windows = (p.rows.T + 31) / 32;
+    const dim3 grid((unsigned)(windows + p.rows.requests), (unsigned)((p.pitch + 16 * RT - 1) / (16 * RT)));
+    adapter_project_tiles_kernel<RT><<<grid, 256, 0, stream>>>(p, (unsigned)windows, dev.xcds > 0 ? dev.xcds : 1);
+    return hipGetLastError();
+}
+
 template <bool TRANSPOSED, int FM>
 hipError_t launch_few(const FewParams& p, dim3 grid, DeviceInfo& dev, hipStream_t stream)
 {
@@ -723,6 +811,13 @@ int adapter_base_split(int64_t M, int64_t N, int64_t K)
     if (tiles <= 0 || tiles >= 256) return 1;
     const int64_t s = 512 / tiles < slices / 4 ? 512 / tiles : slices / 4;
     return s < 2 ? 1 : s > 16 ? 16 : (int)s;
+}
+
+hipError_t launch_adapter_project_tiles(const ProjectParams& p, DeviceInfo& dev, hipStream_t stream)
+{
+    if (p.pitch <= 16) return launch_project_tiles<1>(p, dev, stream);
+    if (p.pitch <= 32) return launch_project_tiles<2>(p, dev, stream);
+    return launch_project_tiles<4>(p, dev, stream);
 }
 
 AdapterFewPlan adapter_few_plan(int64_t M, int64_t N, int64_t K, int64_t factors)
