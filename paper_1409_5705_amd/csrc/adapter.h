@@ -110,9 +110,10 @@ struct AdapterOuterArgs {
     int rank;
     bool bf16;
     int64_t T;
+    float* padded;             // bf16: room for [T][adapter_pitch(rank)] where an H has rows that are no multiple of 16 bytes
     float* partial;            // with adapter_outer_splits > 1: so many times the size of both outputs
 };
-hipError_t launch_adapter_outer(const AdapterOuterArgs& a, hipStream_t stream);
+hipError_t launch_adapter_outer(const AdapterOuterArgs& a, DeviceInfo& dev, hipStream_t stream);
 // Parts that the rows are divided into, C0 and C1 the columns of the two sums.
 int adapter_outer_splits(int64_t C0, int64_t C1, int64_t count, int rank, bool bf16, int64_t T);
 

@@ -2,7 +2,6 @@
 //
 //   project:  H[t][r] = scale_a sum_k X[t][k] F_a[r][k]            (a: the block of row t's request)
 //   join:     out[t][n] = base[t][n] + sum_r H[t][r] F'_a[r][n]    (base: the product with the shared matrix)
-//   outer:    out[a][r][c] = sum_{t of a} H[t][r] G[t][c]          (a block's gradients)
 //
 // Rows of one matrix belong to different blocks, so what one row holds (an infinity, a NaN) never meets another row's sum:
 // a product takes rows of ONE block at a time, and the others' results are dropped, not multiplied by zero.
@@ -14,33 +13,8 @@
 namespace sfb {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float bf16_float(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
-
-// 16 bytes of a row (eight bf16, four fp32).  fp32 rows need not be 16-byte aligned.
-typedef u32x4 u32x4_by_word __attribute__((aligned(4)));
-template <typename T>
-__device__ __forceinline__ u32x4 load_chunk(const T* p)
-{
-    return *reinterpret_cast<const u32x4_by_word*>(p);
-}
-// The same from element k of a row on; what lies at or behind `end` is zero (bf16: a multiple of eight).
-template <typename T>
-__device__ __forceinline__ u32x4 load_chunk(const T* row, int64_t k, int64_t end)
-{
-    u32x4 v = {0u, 0u, 0u, 0u};
-    if (k + 16 / (int)sizeof(T) <= end) return load_chunk(row + k);
-    if (sizeof(T) == 4) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (k + e < end) v[e] = *reinterpret_cast<const uint32_t*>(row + k + e);
-    }
-    return v;
-}
 
 // acc += sum of a 16-byte chunk of each of 16 rows a and 16 rows b: register i of lane (q, c) is row 4 q + i of a, row c of b.
 template <typename T>
@@ -56,7 +30,6 @@ __device__ __forceinline__ floatx4 mfma_chunk(u32x4 a, u32x4 b, floatx4 acc)
     }
 }
 
-constexpr int64_t MAX_BLOCKS = 1 << 22;      // workgroups of a launch (threads of a grid are counted in 32 bits)
 
 // Up to 16 rows of one request against the 16 RT factors 16 RT * blockIdx.y ..; the wavefronts share k.  For few tiles and fp32:
 // what bounds it is how soon everything is on its way, and a wavefront's loads of U k-steps are in flight together.
@@ -198,143 +171,6 @@ __global__ __launch_bounds__(128) void adapter_join_kernel(AdapterJoinArgs p, in
     }
 }
 
-constexpr int OW = 8, WINDOW = 4096;      // wavefronts; rows of which one list is made
-
-struct OuterParams {
-    AdapterOuter sum[2];
-    const int32_t* row_adapter;
-    const int32_t* ranks;
-    int64_t count;
-    int rank;
-    int64_t T, per;            // rows, rows of a split
-    unsigned tiles0, tiles;
-    float* partial;            // with splits: [split][count][rank][C of the first + C of the second]
-};
-
-// A tile of 16 CE columns and 16 RT factors of one block's gradient, over `per` rows of the matrix.  The workgroup lists the
-// block's rows (WINDOW rows of the matrix at a time), its wavefronts take four of them at a time: the fp32 MFMA's k.  Both operands come from memory in the
-// lanes' own order: lane (q, c) loads 16 bytes of row q, columns CE c .. , which are the columns CE c + f of MFMA f.
-template <typename T, int RT>
-__global__ __launch_bounds__(64 * OW, RT == 4 ? 2 : 4) void adapter_outer_kernel(OuterParams p)
-{
-    constexpr int CE = 16 / (int)sizeof(T), U = RT == 1 ? 8 : 4;
-    __shared__ uint16_t list[WINDOW];
-    __shared__ int counts[OW];
-    __shared__ floatx4 part[OW][CE][64];
-    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const unsigned tile = blockIdx.x % p.tiles;
-    const int64_t block = blockIdx.x / p.tiles;
-    const int a = (int)(block % p.count), r0 = (int)(block / p.count) * 16 * RT;
-    const AdapterOuter& sum = p.sum[tile >= p.tiles0 ? 1 : 0];
-    const int64_t c0 = (int64_t)(tile >= p.tiles0 ? tile - p.tiles0 : tile) * (16 * CE) + CE * l16;
-    const int rank = rank_of(p.ranks, p.rank, a);
-
-    floatx4 acc[RT][CE];
-#pragma unroll
-    for (int f = 0; f < RT; ++f)
-#pragma unroll
-        for (int e = 0; e < CE; ++e) acc[f][e] = floatx4{0.f, 0.f, 0.f, 0.f};
-    const int64_t t_begin = (int64_t)blockIdx.y * p.per, t_end = t_begin + p.per < p.T ? t_begin + p.per : p.T;
-    for (int64_t w0 = t_begin; w0 < t_end && r0 < rank; w0 += WINDOW) {
-        // the rows of the window that belong to the block, in their order
-        constexpr int PER = WINDOW / (64 * OW);
-        int found = 0;
-        uint32_t bits = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int64_t t = w0 + tid * PER + i;
-            if (t < t_end && p.row_adapter[t] == a) {
-                bits |= 1u << i;
-                ++found;
-            }
-        }
-        int before = found;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(before, d);
-            if (lane >= d) before += o;
-        }
-        if (lane == 63) counts[wave] = before;
-        before -= found;
-        __syncthreads();
-        int total = 0;
-#pragma unroll
-        for (int w = 0; w < OW; ++w) {
-            const int c = counts[w];
-            if (w < wave) before += c;
-            total += c;
-        }
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (bits >> i & 1) list[before++] = (uint16_t)(tid * PER + i);
-        __syncthreads();
-        for (int i0 = wave * 4 * U; i0 < total; i0 += OW * 4 * U) {
-            u32x4 g[U];
-            float h[U][RT];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int i = i0 + 4 * u + quad;
-                const bool in = i < total;
-                const int64_t t = w0 + list[in ? i : 0];
-                g[u] = u32x4{0u, 0u, 0u, 0u};
-                if (in) g[u] = load_chunk(static_cast<const T*>(sum.G) + t * sum.C, c0, sum.C);
-#pragma unroll
-                for (int f = 0; f < RT; ++f) {
-                    const int r = r0 + 16 * f + l16;
-                    h[u][f] = in && r < rank ? sum.H[t * sum.ldh + r] : 0.f;
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int e = 0; e < CE; ++e) {
-                    const uint32_t w = g[u][sizeof(T) == 2 ? e >> 1 : e];
-                    const float ge = __uint_as_float(sizeof(T) == 4 ? w : (e & 1) ? w & 0xffff0000u : w << 16);
-#pragma unroll
-                    for (int f = 0; f < RT; ++f) acc[f][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(h[u][f], ge, acc[f][e], 0, 0, 0);
-                }
-        }
-        __syncthreads();
-    }
-    float* const out = p.partial ? p.partial + ((int64_t)blockIdx.y * p.count + a) * p.rank * (p.sum[0].C + p.sum[1].C) +
-                                       (tile >= p.tiles0 ? p.rank * p.sum[0].C : 0)
-                                 : sum.out + (int64_t)a * p.rank * sum.C;
-    // register i of lane (q, c): factor 4 q + i, column CE c + e of acc[.][e]
-#pragma unroll
-    for (int f = 0; f < RT; ++f) {
-#pragma unroll
-        for (int e = 0; e < CE; ++e) part[wave][e][lane] = acc[f][e];
-        __syncthreads();
-        for (int e = wave; e < CE; e += OW) {
-            floatx4 s = part[0][e][lane];
-#pragma unroll
-            for (int w = 1; w < OW; ++w) s += part[w][e][lane];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = r0 + 16 * f + 4 * quad + i;
-                if (r < p.rank && c0 + e < sum.C) out[(int64_t)r * sum.C + c0 + e] = r < rank ? s[i] : 0.f;
-            }
-        }
-        __syncthreads();
-    }
-}
-
-// Adds the splits' sums up, in their order.
-__global__ __launch_bounds__(256) void adapter_outer_join_kernel(OuterParams p, int splits)
-{
-    const int64_t first = p.rank * p.sum[0].C, all = first + p.rank * p.sum[1].C, total = p.count * all;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        float v = p.partial[i];
-        for (int s = 1; s < splits; ++s) v += p.partial[s * total + i];
-        const int64_t a = i / all, at = i % all;
-        if (at < first)
-            p.sum[0].out[a * first + at] = v;
-        else
-            p.sum[1].out[a * (all - first) + at - first] = v;
-    }
-}
-
 template <typename T, int RT>
 void project_start(const ProjectParams& p, dim3 grid, unsigned windows, const DeviceInfo& dev, hipStream_t stream)
 {
@@ -359,29 +195,6 @@ hipError_t project_rank(const ProjectParams& p, const DeviceInfo& dev, hipStream
         project_start<T, 2>(p, grid, (unsigned)windows, dev, stream);
     else
         project_start<T, 4>(p, grid, (unsigned)windows, dev, stream);
-    return hipGetLastError();
-}
-
-int outer_rt(int rank) { return rank <= 16 ? 1 : rank <= 32 ? 2 : 4; }
-int64_t outer_blocks(int64_t C0, int64_t C1, int64_t count, int rank, bool bf16)
-{
-    const int64_t width = 16 * (bf16 ? 8 : 4), rt = outer_rt(rank);
-    return ((C0 + width - 1) / width + (C1 + width - 1) / width) * count * ((rank + 16 * rt - 1) / (16 * rt));
-}
-
-template <typename T>
-hipError_t outer_rank(const OuterParams& p, int splits, hipStream_t stream)
-{
-    const int rt = outer_rt(p.rank);
-    const int64_t workgroups = (int64_t)p.tiles * p.count * ((p.rank + 16 * rt - 1) / (16 * rt));
-    if (workgroups > MAX_BLOCKS) return hipErrorInvalidConfiguration;
-    const dim3 blocks((unsigned)workgroups, (unsigned)splits);
-    if (rt == 1)
-        adapter_outer_kernel<T, 1><<<blocks, 64 * OW, 0, stream>>>(p);
-    else if (rt == 2)
-        adapter_outer_kernel<T, 2><<<blocks, 64 * OW, 0, stream>>>(p);
-    else
-        adapter_outer_kernel<T, 4><<<blocks, 64 * OW, 0, stream>>>(p);
     return hipGetLastError();
 }
 
@@ -412,38 +225,6 @@ hipError_t launch_adapter_join(const AdapterJoinArgs& a, hipStream_t stream)
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
-}
-
-// Two workgroups a CU at least, of 512 rows of the matrix at least.
-int adapter_outer_splits(int64_t C0, int64_t C1, int64_t count, int rank, bool bf16, int64_t T)
-{
-    if (count <= 0 || T <= 0) return 1;
-    const int64_t blocks = outer_blocks(C0, C1, count, rank, bf16), s = std::min((512 + blocks - 1) / blocks, T / 512);
-    return s < 2 ? 1 : s > 16 ? 16 : (int)s;
-}
-
-hipError_t launch_adapter_outer(const AdapterOuterArgs& a, hipStream_t stream)
-{
-    if (a.count <= 0) return hipSuccess;
-    const int64_t width = 16 * (a.bf16 ? 8 : 4);
-    OuterParams p = {};
-    p.sum[0] = a.sum[0];
-    p.sum[1] = a.sum[1];
-    p.row_adapter = a.row_adapter;
-    p.ranks = a.ranks;
-    p.count = a.count;
-    p.rank = a.rank;
-    p.T = a.T;
-    p.tiles0 = (unsigned)((a.sum[0].C + width - 1) / width);
-    p.tiles = p.tiles0 + (unsigned)((a.sum[1].C + width - 1) / width);
-    const int splits = adapter_outer_splits(a.sum[0].C, a.sum[1].C, a.count, a.rank, a.bf16, a.T);
-    p.per = (a.T + splits - 1) / splits;
-    p.partial = splits > 1 ? a.partial : nullptr;
-    const hipError_t e = a.bf16 ? outer_rank<uint16_t>(p, splits, stream) : outer_rank<float>(p, splits, stream);
-    if (e != hipSuccess || splits == 1) return e;
-    const int64_t total = a.count * a.rank * (a.sum[0].C + a.sum[1].C);
-    adapter_outer_join_kernel<<<(unsigned)std::min<int64_t>((total + 255) / 256, 4096), 256, 0, stream>>>(p, splits);
-    return hipGetLastError();
 }
 
 }  // namespace sfb

@@ -1,9 +1,52 @@
 // Device functions of the adapter calls' kernels.
 #pragma once
 #include "adapter.h"
-#include "device.h"
+#include "planes.h"
 
 namespace sfb {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr int64_t MAX_BLOCKS = 1 << 22;      // workgroups of a launch (threads of a grid are counted in 32 bits)
+
+// 16 bytes of a row (eight bf16, four fp32).  fp32 rows need not be 16-byte aligned.
+typedef u32x4 u32x4_by_word __attribute__((aligned(4)));
+template <typename T>
+__device__ __forceinline__ u32x4 load_chunk(const T* p)
+{
+    return *reinterpret_cast<const u32x4_by_word*>(p);
+}
+// The same from element k of a row on; what lies at or behind `end` is zero (bf16: a multiple of eight).
+template <typename T>
+__device__ __forceinline__ u32x4 load_chunk(const T* row, int64_t k, int64_t end)
+{
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (k + 16 / (int)sizeof(T) <= end) return load_chunk(row + k);
+    if (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (k + e < end) v[e] = *reinterpret_cast<const uint32_t*>(row + k + e);
+    }
+    return v;
+}
+
+constexpr uint32_t OUT_OF_RANGE = 0x80000000u;
+
+// A buffer descriptor of 2 GiB from base on (raw bytes; reads beyond it give zeros).
+__device__ __forceinline__ u32x4 descriptor(uint64_t at)
+{
+    const uint64_t base = uniform64(at);
+    return u32x4{(uint32_t)base, (uint32_t)(base >> 32), OUT_OF_RANGE, 0x00020000u};
+}
+template <uint32_t OFF>
+__device__ __forceinline__ void buffer_to_lds_16(uint32_t lds_addr, u32x4 rsrc, uint32_t voff)
+{
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_addr), "v"(voff), "s"(rsrc), "n"(OFF)
+                 : "memory", "scc");
+}
 
 // The request of row t, or -1 (empty requests are passed over: the last q with start[q] <= t).  By a whole wavefront: 64
 // probes a step.
@@ -110,22 +153,21 @@ __device__ __forceinline__ bool project_tile(const ProjectParams& p, unsigned wi
 
 // Row t's projections on the factors r .. r + 3 from their sums (in: whether the lane has such a row).
 __device__ __forceinline__ void store_projection(const ProjectParams& p, const ProjectTile& tile, int64_t t, bool in, int r,
-                                                 float __attribute__((ext_vector_type(4))) sum)
+                                                 floatx4 sum)
 {
     if (!in || r >= p.pitch) return;
     const float s = p.rows.scale ? p.rows.scale[tile.a] : 1.f;
     float h[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) h[e] = r + e < tile.rank ? s * sum[e] : 0.f;
-    typedef float vec4 __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<vec4*>(p.H + t * p.pitch + r) = vec4{h[0], h[1], h[2], h[3]};
+    *reinterpret_cast<floatx4*>(p.H + t * p.pitch + r) = floatx4{h[0], h[1], h[2], h[3]};
     if (p.Hx) {
         uint16_t first[4], second[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) two_terms(h[e], first[e], second[e]);
         uint16_t* const at = p.Hx + t * 2 * p.pitch + term_at(r);
-        *reinterpret_cast<uint2*>(at) = uint2{(uint32_t)first[0] | (uint32_t)first[1] << 16, (uint32_t)first[2] | (uint32_t)first[3] << 16};
-        *reinterpret_cast<uint2*>(at + 16) = uint2{(uint32_t)second[0] | (uint32_t)second[1] << 16, (uint32_t)second[2] | (uint32_t)second[3] << 16};
+        *reinterpret_cast<u32x2*>(at) = u32x2{(uint32_t)first[0] | (uint32_t)first[1] << 16, (uint32_t)first[2] | (uint32_t)first[3] << 16};
+        *reinterpret_cast<u32x2*>(at + 16) = u32x2{(uint32_t)second[0] | (uint32_t)second[1] << 16, (uint32_t)second[2] | (uint32_t)second[3] << 16};
     }
     if (p.H_out) {
 #pragma unroll

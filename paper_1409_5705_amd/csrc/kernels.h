@@ -17,6 +17,7 @@ struct DeviceInfo {
     bool fwd_stream_lds_set[6] = {};                     // and of the streaming bf16 forward
     bool adapter_base_lds_set[8] = {};                   // and of the product beside the factor blocks (tile, orientation, split)
     bool adapter_few_lds_set[4] = {};                    // (its form for few rows: rows of a tile, orientation)
+    bool adapter_outer_lds_set[3] = {};                  // (the blocks' gradients: factors of a tile)
     int softmax_wait_polls = 1000;                 // bound of the one-read softmax's wait for a partner's word
 };
 

@@ -28,11 +28,7 @@
 namespace sfb {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 struct BaseParams {
     const uint16_t* A;
@@ -50,21 +46,6 @@ struct BaseParams {
     int count, rank;
     int tiles_m, tiles_n, group_m, num_xcd;
 };
-
-constexpr uint32_t OUT_OF_RANGE = 0x80000000u;
-
-// A buffer descriptor of 2 GiB from base on (raw bytes; reads beyond it give zeros).
-__device__ __forceinline__ u32x4 descriptor(uint64_t at)
-{
-    const uint64_t base = uniform64(at);
-    return u32x4{(uint32_t)base, (uint32_t)(base >> 32), OUT_OF_RANGE, 0x00020000u};
-}
-template <uint32_t OFF>
-__device__ __forceinline__ void buffer_to_lds_16(uint32_t lds_addr, u32x4 rsrc, uint32_t voff)
-{
-    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_addr), "v"(voff), "s"(rsrc), "n"(OFF)
-                 : "memory", "scc");
-}
 
 // The accumulators stay in the accumulation registers: left to itself the compiler moves them to ordinary ones, all at once,
 // for any arithmetic on them, and spills.  The caller sees to it that the MFMAs that wrote them have retired.

@@ -1249,7 +1249,8 @@ int sfb_adapter_backward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J
     o.bf16 = a.bf16;
     o.T = T;
     o.partial = reinterpret_cast<float*>(ctx->ws + l.off_outer);
-    SFB_RUN(KID_ADAPTER_OUTER, sfb::launch_adapter_outer(o, ctx->stream));
+    o.padded = Hw;      // (free where the caller's H is taken)
+    SFB_RUN(KID_ADAPTER_OUTER, sfb::launch_adapter_outer(o, ctx->dev, ctx->stream));
     return SFB_OK;
 }
 
