@@ -355,7 +355,7 @@ typedef struct {
 typedef struct {
     const int64_t* start;   /* [count + 1] device */
     const int32_t* adapter; /* [count] device */
-    int64_t count;          /* requests, >= 0 */
+    int64_t count;          /* requests, 0 .. 1048576 */
 } sfb_requests;
 
 /*
@@ -367,6 +367,7 @@ typedef struct {
  * W, fp32 blocks: the fp32 array (w_dtype SFB_F32).  bf16 blocks: a row-major bf16 array [J][D] (w_dtype SFB_BF16), or the
  * fp32 array that is attached to this context with a bf16 working copy or as two planes (w_dtype SFB_F32): the copy or the
  * high plane is read.  bf16 needs J % 8 == 0 and D % 8 == 0, and takes J and D up to 4194304.
+ * T: up to 16777216.
  *
  * sfb_adapter_backward: the gradients of a loss with dY = d loss / d Y given,
  *       dH[t][r] = scale[a] * sum_j dY[t][j] U_a[r][j]

@@ -186,7 +186,6 @@ template <typename T>
 hipError_t project_rank(const ProjectParams& p, const DeviceInfo& dev, hipStream_t stream)
 {
     const int64_t windows = (p.rows.T + 15) / 16, blocks = windows + p.rows.requests;
-    if (blocks > MAX_BLOCKS) return hipErrorInvalidConfiguration;
     const int rt = p.pitch <= 16 ? 1 : p.pitch <= 32 ? 2 : 4;
     const dim3 grid((unsigned)blocks, (unsigned)std::max(1, (p.pitch + 16 * rt - 1) / (16 * rt)));
     if (rt == 1)
@@ -205,7 +204,7 @@ hipError_t launch_adapter_project(const AdapterProjectArgs& a, DeviceInfo& dev, 
     if (a.rows.T <= 0) return hipSuccess;
     ProjectParams p = {a.rows, a.X, a.F, a.K, a.row_adapter, a.H, a.H_out, a.Hx, adapter_pitch(a.rows.rank)};
     // whole tiles of 32 rows where there are as many as half of the CUs, and rows enough of a request to fill them
-    if (a.bf16 && p.pitch > 0 && a.rows.T >= 16 * (int64_t)dev.cus && a.rows.T >= 16 * a.rows.requests && (a.rows.T + 31) / 32 + a.rows.requests <= MAX_BLOCKS)
+    if (a.bf16 && p.pitch > 0 && a.rows.T >= 16 * (int64_t)dev.cus && a.rows.T >= 16 * a.rows.requests)
         return launch_adapter_project_tiles(p, dev, stream);
     return a.bf16 ? project_rank<uint16_t>(p, dev, stream) : project_rank<float>(p, dev, stream);
 }

@@ -20,6 +20,7 @@ struct OuterParams {
     int rank;
     int64_t T, per;            // rows, rows of a split
     unsigned tiles0, tiles;
+    int64_t first;             // workgroups of the launches before
     int window;                // rows of a list (bf16: their offsets in G have 31 bits)
     float* partial;            // with splits: [split][count][rank][C of the first + C of the second]
 };
@@ -34,8 +35,8 @@ struct OuterTile {
 __device__ __forceinline__ OuterTile outer_tile(const OuterParams& p, int width, int factors)
 {
     OuterTile t;
-    const unsigned tile = blockIdx.x % p.tiles;
-    const int64_t block = blockIdx.x / p.tiles;
+    const unsigned tile = (unsigned)((p.first + blockIdx.x) % p.tiles);
+    const int64_t block = (p.first + blockIdx.x) / p.tiles;
     const bool second = tile >= p.tiles0;
     t.sum = &p.sum[second ? 1 : 0];
     t.a = (int)(block % p.count);
@@ -364,15 +365,18 @@ hipError_t outer_start(const OuterParams& p, dim3 blocks, bool bf16, DeviceInfo&
     adapter_outer_bf16_kernel<RT><<<blocks, 64 * OW, outer_lds(RT), stream>>>(p);
     return hipGetLastError();
 }
-hipError_t outer_rank(const OuterParams& p, int splits, bool bf16, DeviceInfo& dev, hipStream_t stream)
+hipError_t outer_rank(OuterParams p, int splits, bool bf16, DeviceInfo& dev, hipStream_t stream)
 {
     const int rt = outer_rt(p.rank);
     const int64_t workgroups = (int64_t)p.tiles * p.count * ((p.rank + 16 * rt - 1) / (16 * rt));
-    if (workgroups > MAX_BLOCKS) return hipErrorInvalidConfiguration;
-    const dim3 blocks((unsigned)workgroups, (unsigned)splits);
-    if (rt == 1) return outer_start<1>(p, blocks, bf16, dev, stream);
-    if (rt == 2) return outer_start<2>(p, blocks, bf16, dev, stream);
-    return outer_start<4>(p, blocks, bf16, dev, stream);
+    for (p.first = 0; p.first < workgroups; p.first += MAX_BLOCKS) {
+        const dim3 blocks((unsigned)std::min(MAX_BLOCKS, workgroups - p.first), (unsigned)splits);
+        const hipError_t e = rt == 1 ? outer_start<1>(p, blocks, bf16, dev, stream)
+                             : rt == 2 ? outer_start<2>(p, blocks, bf16, dev, stream)
+                                       : outer_start<4>(p, blocks, bf16, dev, stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace

@@ -1021,7 +1021,7 @@ static int check_adapters(int64_t J, int64_t D, int64_t T, const sfb_adapters* a
 {
     constexpr int64_t BF16_COLS = 4194304;      // a tile's rows are addressed with 32-bit offsets
     if (!ad || J <= 0 || D <= 0 || T < 0 || !valid_dtype(ad->dtype)) return SFB_EINVAL;
-    if (T > INT32_MAX || J > INT32_MAX || D > INT32_MAX) return SFB_EINVAL;
+    if (T > (1 << 24) || J > INT32_MAX || D > INT32_MAX) return SFB_EINVAL;
     if (ad->dtype == SFB_BF16 && (J % 8 != 0 || D % 8 != 0 || J > BF16_COLS || D > BF16_COLS)) return SFB_EINVAL;
     if (ad->count < 0 || ad->count > 65536) return SFB_EINVAL;
     if (ad->rank < (ad->count > 0 ? 1 : 0) || ad->rank > SFB_ADAPTER_MAX_RANK) return SFB_EINVAL;
@@ -1074,7 +1074,7 @@ static int check_adapter_call(const sfb_ctx* ctx, const void* W, int32_t w_dtype
     if (rc != SFB_OK) return rc;
     if (ad->count > 0 && (!ad->U || !ad->V || !aligned16(ad->U) || !aligned16(ad->V) || !aligned16(ad->ranks) || !aligned16(ad->scale)))
         return SFB_EINVAL;
-    if (!rq || rq->count < 0 || !aligned16(rq->start) || !aligned16(rq->adapter)) return SFB_EINVAL;
+    if (!rq || rq->count < 0 || rq->count > (1 << 20) || !aligned16(rq->start) || !aligned16(rq->adapter)) return SFB_EINVAL;
     if (rq->count > 0 && (!rq->start || !rq->adapter)) return SFB_EINVAL;
     if (!W || !aligned16(W) || !valid_dtype(w_dtype)) return SFB_EINVAL;
     *Wb = nullptr;

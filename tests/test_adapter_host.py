@@ -54,10 +54,10 @@ def test_refusals_of_both(sfb, ctx, call):
     for a in (dict(U=None), dict(V=None), dict(U=P + 8), dict(V=P + 2), dict(ranks=P + 4), dict(scale=P + 4), dict(count=-1),
               dict(count=65537), dict(rank=0), dict(rank=257), dict(dtype=2), dict(dtype=-1)):
         assert call(sfb, ctx, ad=adapters(sfb, **a)) == sfb.SFB_EINVAL, a
-    for r in (dict(start=None), dict(adapter=None), dict(start=P + 8), dict(adapter=P + 4), dict(count=-1)):
+    for r in (dict(start=None), dict(adapter=None), dict(start=P + 8), dict(adapter=P + 4), dict(count=-1), dict(count=(1 << 20) + 1)):
         assert call(sfb, ctx, rq=requests(sfb, **r)) == sfb.SFB_EINVAL, r
     for k in (dict(W=None), dict(W=P + 8), dict(w_dtype=0), dict(w_dtype=3), dict(J=0), dict(D=-8), dict(J=60), dict(D=60),
-              dict(J=4194312), dict(D=4194312), dict(T=-1), dict(X=None), dict(X=P + 2), dict(H=P + 4), dict(T=1 << 31)):
+              dict(J=4194312), dict(D=4194312), dict(T=-1), dict(X=None), dict(X=P + 2), dict(H=P + 4), dict(T=(1 << 24) + 1)):
         assert call(sfb, ctx, **k) == sfb.SFB_EINVAL, k
     # fp32: any sizes, an fp32 matrix
     assert call(sfb, ctx, ad=adapters(sfb, dtype=0), w_dtype=0, J=61, D=3) == sfb.SFB_ENOWS

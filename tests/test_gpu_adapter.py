@@ -332,3 +332,159 @@ def test_large_offsets(ctx):
     assert float(Y[:-3].float().abs().max()) == 0.0
     del X, V, U, W, Y
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("T,S,J,D,R", [(40, 5, 136, 200, 8), (700, 9, 136, 200, 20), (700, 9, 136, 200, 70)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_infinities_of_the_rows(ctx, dtype, T, S, J, D, R):
+    """An infinity in a row of dY or X is one of the same sign in the gradients it enters, not a not-a-number, and reaches no
+    other block's."""
+    n = 3
+    c = A.make(T, J, D, n, R, S, dtype, seed=T + R, none=0)
+    c["ranks"][:] = R
+    c["adapter"] = (torch.arange(S) % n).to(torch.int32)
+    ref, rows = A.reference(c)
+    by, _ = A.rows_of(c)
+    t = by[1][len(by[1]) // 2]
+    d, o = to_dev(c), outputs(c)
+    forward(ctx, d, o)
+    h = o["H"][t].cpu()
+    assert bool((h != 0).all())
+    d["dY"][t, 17] = float("inf")
+    ctx.sfb_adapter_backward(d["W"], d["X"], d["dY"], d["start"], d["adapter"], d["U"], d["V"], None, o["dU"], o["dV"], ranks=d["ranks"],
+                             scale=d["scale"], H=o["H"])
+    got = o["dU"][1].cpu()
+    assert bool((got[:, 17] == torch.sign(h) * float("inf")).all())
+    keep = torch.ones(J, dtype=torch.bool)
+    keep[17] = False
+    A.check("dU", got[:, keep], {"dU": ref["dU"][1][:, keep.numpy()], "dU_tol": ref["dU_tol"][1][:, keep.numpy()]})
+    for k in ("dU", "dV"):
+        A.check(k, o[k][[0, 2]], {k: ref[k][[0, 2]], k + "_tol": ref[k + "_tol"][[0, 2]]})
+    d = to_dev(c)
+    d["X"][t, 5] = float("-inf")
+    ctx.sfb_adapter_backward(d["W"], d["X"], d["dY"], d["start"], d["adapter"], d["U"], d["V"], None, o["dU"], o["dV"], ranks=d["ranks"],
+                             scale=d["scale"], H=o["H"])
+    dh = float(c["scale"][1]) * (c["dY"][t].double() @ c["U"][1].double().T)
+    assert bool((o["dV"][1][:, 5].cpu() == torch.sign(dh).float() * float("-inf")).all())
+    A.check("dV", o["dV"][[0, 2]], {"dV": ref["dV"][[0, 2]], "dV_tol": ref["dV_tol"][[0, 2]]})
+
+
+@pytest.mark.parametrize("T", [30, 400])
+def test_two_contexts_on_two_streams(sfb, T):
+    """Contexts of their own on side streams, at work at the same time; inputs made on the default stream."""
+    c = A.make(T, 264, 328, 4, 16, 5, BF16, seed=6)
+    ref, rows = A.reference(c)
+    d = to_dev(c)
+    torch.cuda.synchronize()
+    runs = []
+    for _ in range(2):
+        stream = torch.cuda.Stream()
+        own = sfb.Context(0, stream=stream)
+        runs.append((stream, own, outputs(c)))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for stream, own, o in runs:           # the current stream is the default one throughout
+            forward(own, d, o)
+            backward(own, d, o, H=o["H"])
+    torch.cuda.synchronize()
+    for stream, own, o in runs:
+        compare(c, o)
+        own.close()
+
+
+@pytest.mark.parametrize("T", [20, 200, 900])
+@pytest.mark.parametrize("start", [[5, 3, 10, 2], [-7, 4, 2000, 9], [3, 2 ** 40, -2 ** 40, 8], [900, 0, 900, 0]])
+def test_starts_that_are_not_in_order(ctx, T, start):
+    """What start may not hold: the results are unspecified, but nothing in front of and behind the outputs is touched."""
+    c = A.make(T, 72, 136, 3, 20, 3, BF16, seed=9)
+    c["start"] = torch.tensor(start)
+    d = to_dev(c)
+    wide = {}
+    o = {}
+    for k, v in outputs(c).items():
+        wide[k] = torch.full((v.numel() + 1024,), SENTINEL, dtype=v.dtype, device="cuda:0")
+        o[k] = wide[k][512:512 + v.numel()].view(v.shape)
+    forward(ctx, d, o)
+    backward(ctx, d, o, H=o["H"])
+    backward(ctx, d, o)
+    torch.cuda.synchronize()
+    for k, w in wide.items():
+        assert bool((w[:512] == w.new_full((1,), SENTINEL)).all()) and bool((w[-512:] == w.new_full((1,), SENTINEL)).all()), k
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T", [48, 900])
+def test_training_steps(sfb, dtype, T):
+    """Adapters trained beside a frozen matrix, as a program does it: forward, the gradient of a squared error, backward, the norm
+    over the gradients of two projections and their clipping, the step; eagerly and from a graph, each step against 64 bits."""
+    J, D, n, R, S, lr, bound = 72, 136, 3, 6, 4, 0.05, 0.5
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        own = sfb.Context(0)
+        first = A.make(T, D, J, n, R, S, dtype, seed=50)          # J -> D, then D -> J
+        second = A.make(T, J, D, n, R, S, dtype, seed=51)
+        for k in ("start", "adapter", "ranks", "scale"):
+            second[k] = first[k]
+        a, b = to_dev(first), to_dev(second)
+        target = torch.randn(T, J, generator=torch.Generator().manual_seed(3)).to("cuda:0")
+        Ha, Hb = (torch.zeros(T, R, device="cuda:0") for _ in range(2))
+        X1 = torch.zeros(T, D, device="cuda:0", dtype=dtype)
+        Y = torch.zeros(T, J, device="cuda:0", dtype=dtype)
+        dX1, G = torch.zeros_like(X1), torch.zeros_like(Y)
+        grads = [torch.zeros(n, R, k, device="cuda:0") for k in (D, J, J, D)]
+        lst, norm = sfb.TensorList(grads), torch.zeros(1, device="cuda:0")
+        params = [a["U"], a["V"], b["U"], b["V"]]
+        start = [p.clone() for p in params]
+        common = dict(ranks=a["ranks"], scale=a["scale"])
+
+        def step():
+            own.sfb_adapter_forward(a["W"], a["X"], a["start"], a["adapter"], a["U"], a["V"], X1, H=Ha, **common)
+            own.sfb_adapter_forward(b["W"], X1, a["start"], a["adapter"], b["U"], b["V"], Y, H=Hb, **common)
+            G.copy_((Y.float() - target) / T)
+            own.sfb_adapter_backward(b["W"], X1, G, a["start"], a["adapter"], b["U"], b["V"], dX1, grads[2], grads[3], H=Hb, **common)
+            own.sfb_adapter_backward(a["W"], a["X"], dX1, a["start"], a["adapter"], a["U"], a["V"], None, grads[0], grads[1], H=Ha, **common)
+            own.sfb_clip_grads(lst, bound, norm)
+            for p, g in zip(params, grads):
+                p.copy_(p.float() - lr * g)
+
+        def check(before):
+            """The step from `before` by the formulas, each part from the call's own inputs."""
+            c2 = dict(second, X=X1.cpu(), dY=G.cpu(), U=before[2].cpu(), V=before[3].cpu())
+            r2, rows = A.reference(c2)
+            A.check("Y", Y, r2, rows)
+            A.check("dX", dX1, r2, rows)
+            c1 = dict(first, X=a["X"].cpu(), dY=dX1.cpu(), U=before[0].cpu(), V=before[1].cpu())
+            r1, _ = A.reference(c1)
+            A.check("Y", X1, r1, rows)
+            raw = [r1["dU"], r1["dV"], r2["dU"], r2["dV"]]
+            tol = [r1["dU_tol"], r1["dV_tol"], r2["dU_tol"], r2["dV_tol"]]
+            want = np.sqrt(sum((x * x).sum() for x in raw))
+            off = np.sqrt(sum((x * x).sum() for x in tol)) + 2.0 ** -23 * want
+            assert abs(norm.item() - want) <= off and want > bound
+            coef = bound / want
+            for p, q, x, e in zip(params, before, raw, tol):
+                new = q.double().cpu().numpy() - lr * coef * x
+                room = lr * coef * (e + np.abs(x) * (off / want + 2.0 ** -21)) + 2.0 ** -22 * (np.abs(q.double().cpu().numpy()) + np.abs(new))
+                half = 2.0 ** -8 if p.dtype == BF16 else 0.0
+                assert np.all(np.abs(p.double().cpu().numpy() - new) <= room * (1 + half) + half * np.abs(new))
+
+        eager = []
+        for _ in range(3):
+            before = [p.clone() for p in params]
+            step()
+            side.synchronize()
+            check(before)
+            eager.append([p.clone() for p in params])
+        for p, s in zip(params, start):
+            p.copy_(s)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+        for k in range(3):
+            graph.replay()
+            side.synchronize()
+            for p, e in zip(params, eager[k]):
+                assert torch.equal(p, e), k
+            assert torch.isfinite(torch.randn(1 << 16, device="cuda:0").sum()).item()
+    own.close()
