@@ -74,6 +74,14 @@ AdapterFewPlan adapter_few_plan(int64_t M, int64_t N, int64_t K, int64_t factors
 hipError_t launch_adapter_few(const AdapterBase& a, const AdapterFewPlan& plan, const AdapterRows& rows, int32_t* row_adapter, DeviceInfo& dev,
                               hipStream_t stream);
 
+// fp32 matrices with zeros behind their rows and columns (cols_out % 4 == 0; rows_out 0: none), both by one launch.
+struct AdapterPad {
+    const float* src = nullptr;
+    float* dst = nullptr;
+    int64_t rows = 0, cols = 0, rows_out = 0, cols_out = 0;
+};
+hipError_t launch_adapter_pad(const AdapterPad& a, const AdapterPad& b, hipStream_t stream);
+
 // out[t][n] = sum_s planes[s][t][n] + sum_r H[t][r] F_a[r][n] for the rows of requests; out and F [count][rank][N] fp32 or bf16.
 struct AdapterJoinArgs {
     const float* planes;       // [split][T][width]

@@ -171,6 +171,19 @@ __global__ __launch_bounds__(128) void adapter_join_kernel(AdapterJoinArgs p, in
     }
 }
 
+// dst [rows_out][cols_out] = src [rows][cols] and zeros behind it, for two matrices.
+__global__ __launch_bounds__(256) void pad_kernel(AdapterPad a, AdapterPad b, int64_t blocks_a)
+{
+    const bool second = blockIdx.x >= blocks_a;
+    const AdapterPad& m = second ? b : a;
+    const int64_t i = ((int64_t)(second ? blockIdx.x - blocks_a : blockIdx.x) * 256 + threadIdx.x) * 4;      // (cols_out % 4 == 0)
+    if (i >= m.rows_out * m.cols_out) return;
+    const int64_t r = i / m.cols_out, c = i % m.cols_out;
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (r < m.rows) v = load_chunk(m.src + r * m.cols, c, m.cols);
+    *reinterpret_cast<u32x4*>(m.dst + i) = v;
+}
+
 template <typename T, int RT>
 void project_start(const ProjectParams& p, dim3 grid, unsigned windows, const DeviceInfo& dev, hipStream_t stream)
 {
@@ -207,6 +220,14 @@ hipError_t launch_adapter_project(const AdapterProjectArgs& a, DeviceInfo& dev, 
     if (a.bf16 && p.pitch > 0 && a.rows.T >= 16 * (int64_t)dev.cus && a.rows.T >= 16 * a.rows.requests)
         return launch_adapter_project_tiles(p, dev, stream);
     return a.bf16 ? project_rank<uint16_t>(p, dev, stream) : project_rank<float>(p, dev, stream);
+}
+
+hipError_t launch_adapter_pad(const AdapterPad& a, const AdapterPad& b, hipStream_t stream)
+{
+    const int64_t blocks_a = (a.rows_out * a.cols_out + 1023) / 1024, blocks = blocks_a + (b.rows_out * b.cols_out + 1023) / 1024;
+    if (blocks == 0) return hipSuccess;
+    pad_kernel<<<(unsigned)blocks, 256, 0, stream>>>(a, b, blocks_a);
+    return hipGetLastError();
 }
 
 hipError_t launch_adapter_join(const AdapterJoinArgs& a, hipStream_t stream)

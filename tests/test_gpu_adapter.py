@@ -112,9 +112,10 @@ def test_many_tiles(ctx, J, D, n, R, S):
     compare(c, o)
 
 
-@pytest.mark.parametrize("J,D,n,R", [(1003, 2047, 2, 12), (65, 63, 3, 5), (2, 3, 2, 1), (130, 1, 1, 7)])
-def test_fp32_odd_sizes(ctx, J, D, n, R):
-    c = A.poison(A.make(90, J, D, n, R, 4, F32, seed=J, behind=2))
+@pytest.mark.parametrize("T,J,D,n,R", [(90, 1003, 2047, 2, 12), (90, 65, 63, 3, 5), (90, 2, 3, 2, 1), (90, 130, 1, 1, 7),
+                                       (900, 1003, 1001, 2, 12), (1200, 1004, 601, 2, 3), (1200, 601, 1004, 2, 3), (1200, 1002, 603, 2, 3)])
+def test_fp32_odd_sizes(ctx, T, J, D, n, R):
+    c = A.poison(A.make(T, J, D, n, R, 4, F32, seed=J, behind=2))
     d, o = to_dev(c), outputs(c)
     forward(ctx, d, o)
     backward(ctx, d, o)
