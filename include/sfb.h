@@ -389,7 +389,7 @@ int sfb_adapter_backward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J
                          float* dU, float* dV);
 
 /*
- * The global norm of the gradients of a step, and their clipping.  The gradients are a list of tensors (host array; device
+ * The global norm of the gradients of a step, and their clipping.  The gradients are a list of tensors (host array of up to 16777216; device
  * pointers, aligned to their elements, 16 bytes for full speed), fp32 and bf16 mixed:
  *       norm = sqrt(sum_i sum_k g_i[k]^2),      dst_i[k] = src_i[k] * min(1, max_norm / norm).
  * sfb_grad_norm writes *norm (device); it does not look at dst.  sfb_clip_grads does both; dst_i may be src_i (scaled in
@@ -397,6 +397,10 @@ int sfb_adapter_backward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J
  * overlap.  Squares are summed in 64 bits in a fixed order.  max_norm >= 0.  A norm that is not finite is reported as it is,
  * and the scale is then 0 (infinite) or not a number: look at *norm before the gradients are used.
  * Needs the workspace of sfb_grad_norm_workspace_bytes.
+ * table (may be NULL): the list's description in device memory, for lists of more tensors than a launch takes as its arguments
+ * (240, clipping 160): with it a pass is one launch whatever their number.  The caller has sfb_tensor_table_fill write it
+ * for the same list into host memory (sfb_tensor_table_bytes, 8-byte aligned) and copies it to the device, once for as long as
+ * the tensors keep their places.
  */
 typedef struct {
     const void* src;   /* [n] of dtype */
@@ -405,8 +409,10 @@ typedef struct {
     int32_t dtype;     /* sfb_dtype */
 } sfb_tensor;
 int64_t sfb_grad_norm_workspace_bytes(const sfb_tensor* list, int64_t count);
-int sfb_grad_norm(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, float* norm);
-int sfb_clip_grads(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, float max_norm, float* norm);
+int64_t sfb_tensor_table_bytes(int64_t count);
+int sfb_tensor_table_fill(const sfb_tensor* list, int64_t count, void* host);
+int sfb_grad_norm(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, const void* table, float* norm);
+int sfb_clip_grads(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, const void* table, float max_norm, float* norm);
 
 /* Static description of a status code. */
 const char* sfb_strerror(int code);

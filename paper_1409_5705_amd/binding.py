@@ -154,9 +154,13 @@ def lib():
         L.sfb_adapter_backward.restype = ctypes.c_int
         L.sfb_grad_norm_workspace_bytes.argtypes = [pt, i64]
         L.sfb_grad_norm_workspace_bytes.restype = i64
-        L.sfb_grad_norm.argtypes = [vp, pt, i64, vp]
+        L.sfb_tensor_table_bytes.argtypes = [i64]
+        L.sfb_tensor_table_bytes.restype = i64
+        L.sfb_tensor_table_fill.argtypes = [pt, i64, vp]
+        L.sfb_tensor_table_fill.restype = ctypes.c_int
+        L.sfb_grad_norm.argtypes = [vp, pt, i64, vp, vp]
         L.sfb_grad_norm.restype = ctypes.c_int
-        L.sfb_clip_grads.argtypes = [vp, pt, i64, ctypes.c_float, vp]
+        L.sfb_clip_grads.argtypes = [vp, pt, i64, vp, ctypes.c_float, vp]
         L.sfb_clip_grads.restype = ctypes.c_int
         L.sfb_prox_rows.argtypes = [vp, vp, i64, i64, i32]
         L.sfb_prox_rows.restype = ctypes.c_int
@@ -236,8 +240,8 @@ def _ptr(t, name, dtype=None, shape=None):
 
 
 class TensorList:
-    """A list of tensors for sfb_grad_norm and sfb_clip_grads, made once and used for as long as the tensors keep their
-    memory: `src` the gradients (fp32 or bf16, contiguous, any sizes), `dst` where the clipped ones go (None: in place)."""
+    """A list of tensors for sfb_grad_norm and sfb_clip_grads, made once (not while a graph is captured) and used for as long as
+    the tensors keep their memory: `src` the gradients (fp32 or bf16, contiguous, any sizes), `dst` where the clipped ones go (None: in place)."""
 
     def __init__(self, src, dst=None):
         src = list(src)
@@ -261,6 +265,14 @@ class TensorList:
         if need < 0:
             raise SfbError(int(need), "sfb_grad_norm_workspace_bytes")
         self.workspace_bytes = int(need)
+        self.table, self.table_ptr = None, None
+        if self.count > 160:             # more than a launch takes as its arguments: described in device memory
+            host = torch.zeros(int(lib().sfb_tensor_table_bytes(self.count)), dtype=torch.uint8)
+            rc = lib().sfb_tensor_table_fill(self.items, self.count, host.data_ptr())
+            if rc != SFB_OK:
+                raise SfbError(rc, "sfb_tensor_table_fill")
+            self.table = host.to(self.device)        # (waits for the copy: any stream may use it)
+            self.table_ptr = self.table.data_ptr()
 
 
 class Context:
@@ -625,12 +637,12 @@ class Context:
     def sfb_grad_norm(self, tensors: TensorList, norm):
         """Enqueues norm[0] = the global 2-norm of the list's tensors."""
         p = self._list(tensors, norm)
-        self._check(lib().sfb_grad_norm(self._h, tensors.items, tensors.count, p), "sfb_grad_norm")
+        self._check(lib().sfb_grad_norm(self._h, tensors.items, tensors.count, tensors.table_ptr, p), "sfb_grad_norm")
 
     def sfb_clip_grads(self, tensors: TensorList, max_norm, norm):
         """Enqueues norm[0] and dst = src * min(1, max_norm / norm) for every tensor of the list."""
         p = self._list(tensors, norm)
-        self._check(lib().sfb_clip_grads(self._h, tensors.items, tensors.count, float(max_norm), p), "sfb_clip_grads")
+        self._check(lib().sfb_clip_grads(self._h, tensors.items, tensors.count, tensors.table_ptr, float(max_norm), p), "sfb_clip_grads")
 
     def sfb_prox_rows(self, W, mode=SFB_PROX_PROJECT):
         J, D = W.shape

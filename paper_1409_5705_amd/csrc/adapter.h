@@ -126,9 +126,12 @@ hipError_t launch_adapter_outer(const AdapterOuterArgs& a, DeviceInfo& dev, hipS
 int adapter_outer_splits(int64_t C0, int64_t C1, int64_t count, int rank, bool bf16, int64_t T);
 
 // Norm over the tensors of a list and their scaling.  partial: grad_norm_partials(...) + 1 doubles.  Where launch_clip follows
-// (clip), with the same list and `partial`, it may be that which writes *norm.
+// (clip), with the same list and `partial`, it may be that which writes *norm.  table (nullable): what tensor_table_fill wrote
+// for this list, in device memory.
 int64_t grad_norm_partials(const sfb_tensor* list, int64_t count);
-hipError_t launch_grad_norm(const sfb_tensor* list, int64_t count, double* partial, float* norm, bool clip, hipStream_t stream);
-hipError_t launch_clip(const sfb_tensor* list, int64_t count, const double* partial, double max_norm, float* norm, hipStream_t stream);
+int64_t tensor_table_bytes(int64_t count);
+void tensor_table_fill(const sfb_tensor* list, int64_t count, void* host);
+hipError_t launch_grad_norm(const sfb_tensor* list, int64_t count, const void* table, double* partial, float* norm, bool clip, hipStream_t stream);
+hipError_t launch_clip(const sfb_tensor* list, int64_t count, const void* table, const double* partial, double max_norm, float* norm, hipStream_t stream);
 
 }  // namespace sfb

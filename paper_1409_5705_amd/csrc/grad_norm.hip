@@ -16,6 +16,7 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int64_t TARGET = 4096;    // pieces of a whole list, about (1024: a list of 1.7 GB 6 % slower, too few to even out)
+constexpr int64_t MOST = 1 << 23;   // workgroups of a launch
 constexpr int64_t FEW = 8192;       // pieces whose sums every workgroup of the second pass adds up itself
 
 // Tensors of one launch: their description travels as a kernel argument (4 KB of them).
@@ -31,6 +32,15 @@ struct ListParams {
 constexpr uint32_t BF16_FLAG = 0x80000000u;
 typedef ListParams<240, false> NormList;
 typedef ListParams<160, true> ClipList;
+// Any number of tensors in one launch, their description in device memory.
+struct TableParams {
+    const void* const* src;
+    void* const* dst;
+    const uint32_t* first;
+    const uint32_t* tail;
+    int count;
+    int64_t piece;
+};
 
 struct Piece {
     const char* src;
@@ -96,7 +106,8 @@ __device__ __forceinline__ double square(double sum, u32x4 v, bool bf16)
 
 constexpr int AHEAD = 8;            // 16-byte loads of a thread in flight
 
-__global__ __launch_bounds__(256) void grad_norm_kernel(NormList p, double* partial)
+template <typename List>
+__global__ __launch_bounds__(256) void grad_norm_kernel(List p, double* partial)
 {
     const Piece t = piece_at(p, blockIdx.x, false);
     double sum = 0.0;
@@ -141,7 +152,8 @@ __global__ __launch_bounds__(256) void grad_norm_final_kernel(double* partial, i
 }
 
 // norm: null, or where the one workgroup with `writes` puts it (the sum is then made here, of `count` pieces).
-__global__ __launch_bounds__(256) void clip_kernel(ClipList p, const double* partial, int64_t count, double max_norm, float* norm, bool writes)
+template <typename List>
+__global__ __launch_bounds__(256) void clip_kernel(List p, const double* partial, int64_t count, double max_norm, float* norm, bool writes)
 {
     const uint32_t block = gridDim.x - 1 - blockIdx.x;      // what the first pass has read last is still in the caches
     const Piece t = piece_at(p, block, true);
@@ -192,6 +204,12 @@ int64_t piece_of(const sfb_tensor* list, int64_t count)
     return per <= 4096 ? 4096 : per <= (1 << 30) ? (per + 4095) / 4096 * 4096 : 1 << 30;
 }
 
+// Last piece of a tensor of n elements, and its type.
+uint32_t tail_of(const sfb_tensor& t, int64_t pieces, int64_t piece)
+{
+    return (uint32_t)(t.n - (pieces - 1) * piece) | (t.dtype == SFB_BF16 ? BF16_FLAG : 0u);
+}
+
 // run(list, workgroups, first workgroup of the launch) for every launch that a list takes.
 template <int N, bool CLIP, typename F>
 hipError_t for_list(const sfb_tensor* list, int64_t count, F&& run)
@@ -215,14 +233,58 @@ hipError_t for_list(const sfb_tensor* list, int64_t count, F&& run)
         const int64_t pieces = (list[i].n + p.piece - 1) / p.piece;
         p.src[k] = list[i].src;
         if (CLIP) p.dst[k] = list[i].dst;
-        p.tail[k] = (uint32_t)(list[i].n - (pieces - 1) * p.piece) | (list[i].dtype == SFB_BF16 ? BF16_FLAG : 0u);
+        p.tail[k] = tail_of(list[i], pieces, p.piece);
         p.first[k] = blocks;
         blocks += (uint32_t)pieces;
     }
     return hipSuccess;
 }
 
+TableParams table_params(const sfb_tensor* list, int64_t count, const void* table)
+{
+    TableParams p = {};
+    for (int64_t i = 0; i < count; ++i) p.count += list[i].n > 0;
+    const char* at = static_cast<const char*>(table);
+    p.src = reinterpret_cast<const void* const*>(at);
+    p.dst = reinterpret_cast<void* const*>(at + 8 * count);
+    p.first = reinterpret_cast<const uint32_t*>(at + 16 * count);
+    p.tail = p.first + count + 1;
+    p.piece = piece_of(list, count);
+    return p;
+}
+
 }  // namespace
+
+int64_t tensor_table_bytes(int64_t count) { return 24 * count + 4; }
+
+void tensor_table_fill(const sfb_tensor* list, int64_t count, void* host)
+{
+    char* const at = static_cast<char*>(host);
+    const void** const src = reinterpret_cast<const void**>(at);
+    void** const dst = reinterpret_cast<void**>(at + 8 * count);
+    uint32_t* const first = reinterpret_cast<uint32_t*>(at + 16 * count);
+    uint32_t* const tail = first + count + 1;
+    const int64_t piece = piece_of(list, count);
+    uint32_t blocks = 0;
+    int64_t k = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        if (list[i].n == 0) continue;
+        const int64_t pieces = (list[i].n + piece - 1) / piece;
+        src[k] = list[i].src;
+        dst[k] = list[i].dst;
+        tail[k] = tail_of(list[i], pieces, piece);
+        first[k++] = blocks;
+        blocks += (uint32_t)pieces;
+    }
+    for (; k <= count; ++k) {      // (behind the tensors that have elements)
+        first[k] = blocks;
+        if (k < count) {
+            src[k] = nullptr;
+            dst[k] = nullptr;
+            tail[k] = 0;
+        }
+    }
+}
 
 int64_t grad_norm_partials(const sfb_tensor* list, int64_t count)
 {
@@ -232,24 +294,34 @@ int64_t grad_norm_partials(const sfb_tensor* list, int64_t count)
     return blocks;
 }
 
-hipError_t launch_grad_norm(const sfb_tensor* list, int64_t count, double* partial, float* norm, bool clip, hipStream_t stream)
+hipError_t launch_grad_norm(const sfb_tensor* list, int64_t count, const void* table, double* partial, float* norm, bool clip, hipStream_t stream)
 {
-    const hipError_t e = for_list<240, false>(list, count, [&](const NormList& p, uint32_t blocks, int64_t done) {
-        grad_norm_kernel<<<blocks, 256, 0, stream>>>(p, partial + done);
-        return hipGetLastError();
-    });
-    if (e != hipSuccess) return e;
     const int64_t pieces = grad_norm_partials(list, count);
-    if (clip && pieces > 0 && pieces <= FEW) return hipSuccess;
-    grad_norm_final_kernel<<<1, 256, 0, stream>>>(partial, pieces, norm);
+    if (table && pieces > 0 && pieces <= MOST) {
+        const TableParams p = table_params(list, count, table);
+        grad_norm_kernel<TableParams><<<(unsigned)pieces, 256, 0, stream>>>(p, partial);
+    } else {
+        const hipError_t e = for_list<240, false>(list, count, [&](const NormList& p, uint32_t blocks, int64_t done) {
+            grad_norm_kernel<NormList><<<blocks, 256, 0, stream>>>(p, partial + done);
+            return hipGetLastError();
+        });
+        if (e != hipSuccess) return e;
+    }
+    if (!(clip && pieces > 0 && pieces <= FEW)) grad_norm_final_kernel<<<1, 256, 0, stream>>>(partial, pieces, norm);
     return hipGetLastError();
 }
 
-hipError_t launch_clip(const sfb_tensor* list, int64_t count, const double* partial, double max_norm, float* norm, hipStream_t stream)
+hipError_t launch_clip(const sfb_tensor* list, int64_t count, const void* table, const double* partial, double max_norm, float* norm, hipStream_t stream)
 {
     const int64_t pieces = grad_norm_partials(list, count);
+    float* const own = pieces <= FEW ? norm : nullptr;
+    if (table && pieces > 0 && pieces <= MOST) {
+        const TableParams p = table_params(list, count, table);
+        clip_kernel<TableParams><<<(unsigned)pieces, 256, 0, stream>>>(p, partial, pieces, max_norm, own, own != nullptr);
+        return hipGetLastError();
+    }
     return for_list<160, true>(list, count, [&](const ClipList& p, uint32_t blocks, int64_t done) {
-        clip_kernel<<<blocks, 256, 0, stream>>>(p, partial, pieces, max_norm, pieces <= FEW ? norm : nullptr, pieces <= FEW && done == 0);
+        clip_kernel<ClipList><<<blocks, 256, 0, stream>>>(p, partial, pieces, max_norm, own, own && done == 0);
         return hipGetLastError();
     });
 }

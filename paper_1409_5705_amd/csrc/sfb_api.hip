@@ -1290,7 +1290,7 @@ int sfb_adapter_backward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J
 
 static int check_list(const sfb_tensor* list, int64_t count, bool clip)
 {
-    if (count < 0 || (count > 0 && !list)) return SFB_EINVAL;
+    if (count < 0 || count > (1 << 24) || (count > 0 && !list)) return SFB_EINVAL;
     for (int64_t i = 0; i < count; ++i) {
         const sfb_tensor& t = list[i];
         if (t.n < 0 || t.n > (int64_t(1) << 48) || !valid_dtype(t.dtype)) return SFB_EINVAL;
@@ -1308,29 +1308,40 @@ int64_t sfb_grad_norm_workspace_bytes(const sfb_tensor* list, int64_t count)
     return rc != SFB_OK ? rc : round_up((sfb::grad_norm_partials(list, count) + 1) * 8);
 }
 
-static int grad_norm_impl(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, bool clip, float max_norm, float* norm)
+int64_t sfb_tensor_table_bytes(int64_t count) { return count < 0 || count > (1 << 24) ? SFB_EINVAL : round_up(sfb::tensor_table_bytes(count)); }
+
+int sfb_tensor_table_fill(const sfb_tensor* list, int64_t count, void* host)
 {
-    if (!ctx || !norm || (reinterpret_cast<uintptr_t>(norm) & 3u)) return SFB_EINVAL;
+    const int rc = check_list(list, count, false);
+    if (rc != SFB_OK) return rc;
+    if (!host || (reinterpret_cast<uintptr_t>(host) & 7u)) return SFB_EINVAL;
+    sfb::tensor_table_fill(list, count, host);
+    return SFB_OK;
+}
+
+static int grad_norm_impl(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, const void* table, bool clip, float max_norm, float* norm)
+{
+    if (!ctx || !norm || (reinterpret_cast<uintptr_t>(norm) & 3u) || !aligned16(table)) return SFB_EINVAL;
     const int rc = check_list(list, count, clip);
     if (rc != SFB_OK) return rc;
     if (!ctx->ws || ctx->ws_bytes < round_up((sfb::grad_norm_partials(list, count) + 1) * 8)) return SFB_ENOWS;
     const DeviceScope scope(ctx->device);
     SFB_TRY(scope.status);
     double* partial = reinterpret_cast<double*>(ctx->ws);
-    SFB_RUN(KID_GRAD_NORM, sfb::launch_grad_norm(list, count, partial, norm, clip, ctx->stream));
-    if (clip) SFB_RUN(KID_CLIP, sfb::launch_clip(list, count, partial, (double)max_norm, norm, ctx->stream));
+    SFB_RUN(KID_GRAD_NORM, sfb::launch_grad_norm(list, count, table, partial, norm, clip, ctx->stream));
+    if (clip) SFB_RUN(KID_CLIP, sfb::launch_clip(list, count, table, partial, (double)max_norm, norm, ctx->stream));
     return SFB_OK;
 }
 
-int sfb_grad_norm(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, float* norm)
+int sfb_grad_norm(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, const void* table, float* norm)
 {
-    return grad_norm_impl(ctx, list, count, false, 0.f, norm);
+    return grad_norm_impl(ctx, list, count, table, false, 0.f, norm);
 }
 
-int sfb_clip_grads(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, float max_norm, float* norm)
+int sfb_clip_grads(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, const void* table, float max_norm, float* norm)
 {
     if (!(max_norm >= 0.f)) return SFB_EINVAL;
-    return grad_norm_impl(ctx, list, count, true, max_norm, norm);
+    return grad_norm_impl(ctx, list, count, table, true, max_norm, norm);
 }
 
 const char* sfb_strerror(int code)

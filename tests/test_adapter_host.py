@@ -99,16 +99,41 @@ def test_refusals_of_clipping(sfb, ctx):
         return t, len(rows)
 
     good = [(P, P, 5, 0), (P + 2, P + 2, 9, 1), (None, None, 0, 1)]
-    assert L.sfb_grad_norm(ctx, *items(*good), P) == sfb.SFB_ENOWS
-    assert L.sfb_clip_grads(ctx, *items(*good), 1.0, P) == sfb.SFB_ENOWS
-    assert L.sfb_grad_norm(ctx, *items((P, None, 5, 0)), P) == sfb.SFB_ENOWS          # dst is not looked at
-    assert L.sfb_clip_grads(ctx, *items((P, None, 5, 0)), 1.0, P) == sfb.SFB_EINVAL
+    assert L.sfb_grad_norm(ctx, *items(*good), None, P) == sfb.SFB_ENOWS
+    assert L.sfb_clip_grads(ctx, *items(*good), None, 1.0, P) == sfb.SFB_ENOWS
+    assert L.sfb_grad_norm(ctx, *items((P, None, 5, 0)), None, P) == sfb.SFB_ENOWS          # dst is not looked at
+    assert L.sfb_clip_grads(ctx, *items((P, None, 5, 0)), None, 1.0, P) == sfb.SFB_EINVAL
     for bad in ((None, P, 5, 0), (P + 2, P, 5, 0), (P + 1, P, 5, 1), (P, P, -1, 0), (P, P, 5, 2)):
-        assert L.sfb_grad_norm(ctx, *items(bad), P) == sfb.SFB_EINVAL, bad
+        assert L.sfb_grad_norm(ctx, *items(bad), None, P) == sfb.SFB_EINVAL, bad
         assert L.sfb_grad_norm_workspace_bytes(*items(bad)) == sfb.SFB_EINVAL
     for bound in (-1.0, float("nan")):
-        assert L.sfb_clip_grads(ctx, *items(*good), bound, P) == sfb.SFB_EINVAL
-    assert L.sfb_grad_norm(None, *items(*good), P) == sfb.SFB_EINVAL
-    assert L.sfb_grad_norm(ctx, *items(*good), None) == sfb.SFB_EINVAL
-    assert L.sfb_grad_norm(ctx, None, 1, P) == sfb.SFB_EINVAL and L.sfb_grad_norm(ctx, None, -1, P) == sfb.SFB_EINVAL
+        assert L.sfb_clip_grads(ctx, *items(*good), None, bound, P) == sfb.SFB_EINVAL
+    assert L.sfb_grad_norm(None, *items(*good), None, P) == sfb.SFB_EINVAL
+    assert L.sfb_grad_norm(ctx, *items(*good), None, None) == sfb.SFB_EINVAL
+    assert L.sfb_grad_norm(ctx, None, 1, None, P) == sfb.SFB_EINVAL and L.sfb_grad_norm(ctx, None, -1, None, P) == sfb.SFB_EINVAL
     assert L.sfb_grad_norm_workspace_bytes(None, 0) > 0
+    assert L.sfb_grad_norm(ctx, *items(*good), P + 8, P) == sfb.SFB_EINVAL
+    assert L.sfb_tensor_table_bytes(-1) == sfb.SFB_EINVAL and L.sfb_tensor_table_bytes(10) >= 10 * 24
+    room = ctypes.create_string_buffer(4096)
+    at = (ctypes.addressof(room) + 15) // 16 * 16
+    assert L.sfb_tensor_table_fill(*items(*good), None) == sfb.SFB_EINVAL and L.sfb_tensor_table_fill(*items(*good), at + 4) == sfb.SFB_EINVAL
+    assert L.sfb_tensor_table_fill(*items((P, P, -1, 0)), at) == sfb.SFB_EINVAL
+    assert L.sfb_tensor_table_fill(*items(*good), at) == sfb.SFB_OK
+
+
+def test_table_of_a_list(sfb):
+    """src and dst of the tensors that have elements, the first workgroup of each, the elements of its last piece and its type."""
+    L = sfb.lib()
+    sizes = [5, 0, 4096, 4097, 0, 9000, 1]
+    t = (sfb.binding.sfb_tensor * len(sizes))()
+    for k, n in enumerate(sizes):
+        t[k].src, t[k].dst, t[k].n, t[k].dtype = P * (k + 1), P * (k + 1) + 16, n, k % 2
+    raw = (ctypes.c_uint64 * (L.sfb_tensor_table_bytes(len(sizes)) // 8))()
+    assert L.sfb_tensor_table_fill(t, len(sizes), ctypes.addressof(raw)) == sfb.SFB_OK
+    there = [k for k, n in enumerate(sizes) if n]
+    assert [raw[i] for i in range(5)] == [P * (k + 1) for k in there]
+    assert [raw[7 + i] for i in range(5)] == [P * (k + 1) + 16 for k in there]
+    words = ctypes.cast(ctypes.addressof(raw) + 16 * 7, ctypes.POINTER(ctypes.c_uint32))
+    assert [words[i] for i in range(8)] == [0, 1, 2, 4, 7, 8, 8, 8]
+    bf16 = 1 << 31
+    assert [words[8 + i] for i in range(5)] == [5, 4096, 1 | bf16, 808 | bf16, 1]

@@ -87,6 +87,57 @@ def test_norm_and_clip(sfb, ctx, which):
     assert torch.equal(again, norm)
 
 
+@pytest.mark.parametrize("count", [700, 9000])
+@pytest.mark.parametrize("table", [True, False])
+def test_many_tensors(sfb, ctx, count, table):
+    """More tensors than a launch takes as its arguments, described in device memory or in several launches; more pieces than
+    the scaling pass adds up itself."""
+    flat = torch.randn(count * 8, generator=torch.Generator(device="cuda:0").manual_seed(count), device="cuda:0")
+    out = torch.full_like(flat, 7.0)
+    src = [flat[8 * k:8 * k + 1 + k % 8] for k in range(count)]
+    dst = [out[8 * k:8 * k + 1 + k % 8] for k in range(count)]
+    inside = torch.arange(8, device="cuda:0")[None, :] <= (torch.arange(count, device="cuda:0") % 8)[:, None]
+    want = math.sqrt(float((flat.view(count, 8).double() * inside).square().sum()))
+    lst, norm = sfb.TensorList(src, dst), torch.zeros(1, device="cuda:0")
+    assert lst.table is not None
+    if not table:
+        lst.table_ptr = None
+    ctx.sfb_grad_norm(lst, norm)
+    assert abs(norm.item() - want) <= 2.0 ** -24 * want * 1.001
+    ctx.sfb_clip_grads(lst, 0.5 * want, norm.zero_())
+    assert abs(norm.item() - want) <= 2.0 ** -24 * want * 1.001
+    check_clipped([flat[inside.view(-1)]], [out[inside.view(-1)]], 0.5)
+    assert bool((out.view(count, 8)[~inside] == 7.0).all())
+
+
+def test_graph_replays(sfb):
+    """Norm and clipping captured once, replayed on other values, against the eager calls."""
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        own = sfb.Context(0)
+        src = tensors([7, 5000, 70001, 33] * 60, 5)
+        dst = [torch.zeros_like(t) for t in src]
+        lst, norm = sfb.TensorList(src, dst), torch.zeros(1, device="cuda:0")
+        own.sfb_clip_grads(lst, 1.0, norm)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            own.sfb_clip_grads(lst, 1.0, norm)
+        for k in range(3):
+            for t, new in zip(src, tensors([7, 5000, 70001, 33] * 60, 6 + k)):
+                t.copy_(new)
+            for t in dst:
+                t.zero_()
+            graph.replay()
+            side.synchronize()
+            got = [norm.clone()] + [t.clone() for t in dst]
+            own.sfb_clip_grads(lst, 1.0, norm)
+            side.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, [norm] + dst))
+            assert abs(norm.item() - norm64(src)) <= 2.0 ** -23 * norm.item()
+        own.close()
+
+
 def test_empty_list(sfb, ctx):
     norm = torch.full((1,), -1.0, device="cuda:0")
     ctx.sfb_grad_norm(sfb.TensorList([]), norm)
