@@ -116,11 +116,13 @@ __global__ __launch_bounds__(128) void adapter_join_kernel(AdapterJoinArgs p, in
     if (a >= 0 && a < p.count) {
         rank = rank_of(p.ranks, p.rank, a);
         const float scale = p.scale ? p.scale[a] : 1.f;
-        for (int r = threadIdx.x; r < rank; r += 128) {
+        // (all of the row's, those that are not in use too: their number is still on its way)
+        for (int r = threadIdx.x; r < p.rank; r += 128) {
             float h;
             if (p.dense) {
                 h = 0.f;
                 const float* from = p.planes + t * p.width + p.N + (int64_t)a * p.rank + r;
+#pragma unroll 4
                 for (int s = 0; s < p.split; ++s) h += from[s * (p.T * p.width)];
                 h *= scale;
             } else {

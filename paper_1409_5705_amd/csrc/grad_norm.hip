@@ -77,15 +77,17 @@ __device__ __forceinline__ float element(const Piece& p, int64_t i)
 
 __device__ __forceinline__ float scaled(float v, double coef) { return (float)((double)v * coef); }
 
+template <int WAVES>
 __device__ __forceinline__ double block_sum(double v)
 {
-    __shared__ double part[4];
+    __shared__ double part[WAVES];
 #pragma unroll
     for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = part[0] + part[1] + part[2] + part[3];
-    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v += part[w];
     return v;
 }
 
@@ -130,21 +132,23 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(List p, double* partial)
         const double x = (double)element(t, i);
         sum = fma(x, x, sum);
     }
-    sum = block_sum(sum);
+    sum = block_sum<4>(sum);
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
+template <int WAVES>
 __device__ __forceinline__ double sum_of(const double* partial, int64_t count)
 {
     double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < count; i += 256) sum += partial[i];
-    return block_sum(sum);
+#pragma unroll 8
+    for (int64_t i = threadIdx.x; i < count; i += 64 * WAVES) sum += partial[i];
+    return block_sum<WAVES>(sum);
 }
 
 // partial[count] = the sum of the `count` before it; *norm its root.
-__global__ __launch_bounds__(256) void grad_norm_final_kernel(double* partial, int64_t count, float* norm)
+__global__ __launch_bounds__(1024) void grad_norm_final_kernel(double* partial, int64_t count, float* norm)
 {
-    const double sum = sum_of(partial, count);
+    const double sum = sum_of<16>(partial, count);
     if (threadIdx.x == 0) {
         partial[count] = sum;
         *norm = (float)sqrt(sum);
@@ -157,7 +161,7 @@ __global__ __launch_bounds__(256) void clip_kernel(List p, const double* partial
 {
     const uint32_t block = gridDim.x - 1 - blockIdx.x;      // what the first pass has read last is still in the caches
     const Piece t = piece_at(p, block, true);
-    const double total = sqrt(norm ? sum_of(partial, count) : partial[count]);
+    const double total = sqrt(norm ? sum_of<4>(partial, count) : partial[count]);
     if (writes && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)total;
     // (a norm that is no number: neither is this; in 64 bits, since an fp32 scale below 1e-38 would lose its digits)
     const double coef = total <= max_norm ? 1.0 : max_norm / total;
@@ -307,7 +311,7 @@ hipError_t launch_grad_norm(const sfb_tensor* list, int64_t count, const void* t
         });
         if (e != hipSuccess) return e;
     }
-    if (!(clip && pieces > 0 && pieces <= FEW)) grad_norm_final_kernel<<<1, 256, 0, stream>>>(partial, pieces, norm);
+    if (!(clip && pieces > 0 && pieces <= FEW)) grad_norm_final_kernel<<<1, 1024, 0, stream>>>(partial, pieces, norm);
     return hipGetLastError();
 }
 

@@ -213,7 +213,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
         const int r = wm0 + 16 * (t % TM) + l16, rn = wn0 + 16 * (t % TN) + l16;
         ra[t] = (uint32_t)(r * 128 + ((quad ^ swz(r)) << 4));
         rb[t] = A_BYTES + (TRANSPOSED ? transposed_at(t, 8 * quad + (l16 >> 2)) : (uint32_t)(rn * 128 + ((quad ^ swz(rn)) << 4)));
-        rf[t] = F_OFF + transposed_at(t, 8 * (quad & 1) + (l16 >> 2));
+        rf[t] = transposed_at(t, 8 * (quad & 1) + (l16 >> 2));
     }
     struct Frags {
         bf16x8 a[TM];
@@ -251,8 +251,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
     floatx4 acc[TM][TN];
     int mine[TM];                     // block of the lane's row of each MFMA tile
 
-    // ---- the blocks' part of a tile; whether a factor is not finite
-    auto blocks_part = [&](int64_t m0, int64_t n0) {
+    // ---- the blocks' part of a tile, with room for `slots` chunks of their factors from `region` of the LDS on; whether a factor
+    // is not finite
+    auto blocks_part = [&](int64_t m0, int64_t n0, uint32_t region, int slots) {
         bool special = false;         // whether the wavefront has met a factor that is not finite
         const int lane = here(threadIdx.x & 63), l16 = lane & 15, quad = lane >> 4, wave = here_scalar(wave0);
         uint64_t left[TBM / 64];      // rows of the tile whose block is still to come
@@ -273,7 +274,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
         }
         u32x4 h[TM];
         int h_from = -1;
-        // Rounds of four chunks of 16 pairs, the first 16 of all blocks and then the next: LDS rows of TBN columns as W's, transposed.
+        // Rounds of `slots` chunks of 16 pairs, the first 16 of all blocks and then the next: LDS rows of TBN columns as W's, transposed.
         // Lane k knows the k-th chunk's block, first pair and the block's rank.
         uint64_t all[TBM / 64];
 #pragma unroll
@@ -281,7 +282,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
         int cur_r = 0;
         for (;;) {
             int of = -1, from = 0, ranks = 0, chunks = 0;
-            while (chunks < 4 && cur_r < p.rank) {
+            while (chunks < slots && cur_r < p.rank) {
                 int a = -1;
 #pragma unroll
                 for (int i = 0; i < TBM / 64; ++i)
@@ -316,7 +317,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
                     constexpr int PER = (int)(F_CHUNK / 4096);
                     const int r = (PER * wave + decltype(I)::value) * RPL + lane / SLOTS, u = (lane % SLOTS) ^ ((r & 3) << 2);
                     const bool in = r0 + r < rank && n0 + 8 * u < p.N;
-                    buffer_to_lds_16<decltype(I)::value * 1024u>(lds_base + F_OFF + (uint32_t)k * F_CHUNK + (uint32_t)(PER * wave) * 1024u, descriptor(factors),
+                    buffer_to_lds_16<decltype(I)::value * 1024u>(lds_base + region + (uint32_t)k * F_CHUNK + (uint32_t)(PER * wave) * 1024u, descriptor(factors),
                                                                in ? (uint32_t)r * (uint32_t)(p.N * 2) + (uint32_t)u * 16u : OUT_OF_RANGE);
                 });
             }
@@ -340,7 +341,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
                     uint32_t least = 0x7f807f80u;      // of both halves; 0: not finite
 #pragma unroll
                     for (int t = 0; t < TN; ++t) {
-                        const char* const at = lds + rf[t >> 1] + c * F_CHUNK + (t & 1) * 8;
+                        const char* const at = lds + region + rf[t >> 1] + c * F_CHUNK + (t & 1) * 8;
                         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
                         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * (TBN * 2)));
                         f[t] = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -440,16 +441,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
 
     // ---- pipeline: slice s lives in stage s & 1; f0 holds the fragments of its first k-step, f1 of the second
     Frags f0, f1;
-    enter_tile(0);
+    // Small tiles: the first one's blocks come in front of its slices and have all of the LDS for their factors (704 rows, 8192 x
+    // 2048, 40 requests with blocks of 32 pairs: 46 us, with four chunks a round 49).  (On the large ones the order costs registers.)
+    constexpr bool FIRST = TM == 4 && !SPLIT;
+    auto prologue = [&]() {
+        enter_tile(0);
 #pragma unroll 1
-    for (int s = 0; s < 2; ++s) {
-        static_for<0, LOADS>(issue_one);
-        issue_done();
-    }
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
-    __syncthreads();
+        for (int s = 0; s < 2; ++s) {
+            static_for<0, LOADS>(issue_one);
+            issue_done();
+        }
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < READS; ++i) read_one(f0, 0, i);
+        for (int i = 0; i < READS; ++i) read_one(f0, 0, i);
+    };
+    if constexpr (!FIRST) prologue();
 
     auto slice_body = [&]() {
         auto mfma = [&](const Frags& f, auto J) {
@@ -499,9 +506,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
                 const int64_t m = m0 + wm0 + 16 * ta + l16;
                 mine[ta] = m < p.M ? p.row_adapter[m] : ROW_OUTSIDE;
             }
-            special = blocks_part(m0, n0);
+            const bool all = FIRST && t == 0;
+            special = blocks_part(m0, n0, all ? 0u : F_OFF, all ? (int)((F_OFF + 4 * F_CHUNK) / F_CHUNK) : 4);
             // (vmcnt(0): a load that nobody has waited for, one of H, would have the compiler wait in every slice)
             __builtin_amdgcn_s_waitcnt(0x0f70);
+            if (FIRST && t == 0) {
+                __syncthreads();                           // (the chunks have been read)
+                prologue();
+            }
         }
 #pragma unroll
         for (int ta = 0; ta < TM; ++ta)
