@@ -411,7 +411,7 @@ hipError_t launch_adapter_outer(const AdapterOuterArgs& a, DeviceInfo& dev, hipS
         const int64_t widest = std::max(a.sum[0].C, a.sum[1].C), most = (int64_t(1) << 30) / widest;
         if (most < WINDOW) p.window = (int)(most < 64 ? 64 : most / 64 * 64);
         for (int i = 0; i < 2; ++i) {      // (16-byte pieces of H's rows)
-            if (p.sum[i].ldh % 4 == 0) continue;
+            if (p.sum[i].ldh % 4 == 0 || a.T == 0) continue;
             const int pitch = adapter_pitch(a.rank);
             const int64_t total = a.T * pitch;
             pad_projections_kernel<<<(unsigned)std::min<int64_t>((total + 255) / 256, 2048), 256, 0, stream>>>(p.sum[i].H, a.padded, a.rank, pitch, total);

@@ -102,7 +102,7 @@ def test_forward_and_backward(ctx, case, dtype):
     assert bool((q["H"] == SENTINEL).all())
 
 
-@pytest.mark.parametrize("J,D,n,R,S", [(4104, 72, 5, 24, 9), (72, 4104, 5, 24, 9), (4104, 136, 30, 70, 300), (200, 4360, 30, 70, 300)])
+@pytest.mark.parametrize("J,D,n,R,S", [(4104, 72, 5, 24, 9), (72, 4104, 5, 24, 9), (4104, 136, 30, 70, 300), (200, 4360, 30, 70, 300), (264, 328, 5, 70, 9), (4360, 328, 5, 7, 20)])
 def test_many_tiles(ctx, J, D, n, R, S):
     """Outputs of more tiles than the chip has compute units, rows of no request in the first and in the last ones."""
     c = A.poison(A.make(4200, J, D, n, R, S, BF16, seed=J + S, first=3, behind=260))
@@ -122,7 +122,7 @@ def test_fp32_odd_sizes(ctx, T, J, D, n, R):
     compare(c, o)
 
 
-@pytest.mark.parametrize("T,J,D,n,R,S", [(0, 64, 64, 2, 4, 0), (9, 64, 64, 2, 4, 0), (9, 64, 72, 0, 4, 3), (40, 64, 64, 3, 4, 8)])
+@pytest.mark.parametrize("T,J,D,n,R,S", [(0, 64, 64, 2, 4, 0), (9, 64, 64, 2, 4, 0), (9, 64, 64, 2, 7, 0), (9, 64, 72, 0, 4, 3), (40, 64, 64, 3, 4, 8), (300, 64, 64, 3, 5, 8)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_nothing_there(ctx, T, J, D, n, R, S, dtype):
     """No rows, no requests, no blocks, blocks of rank 0: outputs of rows that belong to requests are the shared matrix's alone,
@@ -136,6 +136,8 @@ def test_nothing_there(ctx, T, J, D, n, R, S, dtype):
     d, o = to_dev(c), outputs(c)
     forward(ctx, d, o)
     backward(ctx, d, o)
+    compare(c, o)
+    backward(ctx, d, o, H=torch.zeros_like(o["H"]))          # (nothing of H is in use either)
     compare(c, o)
 
 
