@@ -64,7 +64,6 @@ int adapter_base_split(int64_t M, int64_t N, int64_t K);
 
 // The same for few rows: planes alone, of `width` columns; with `dense` those behind the N of the product are A times the
 // factors of all blocks ([count][rank][K]).  row_adapter (nullable): written as launch_adapter_project does.
-constexpr int64_t FEW_ROWS = 256;
 struct AdapterFewPlan {
     bool few = false, dense = false;
     int split = 1, tile_m = 64;
@@ -112,7 +111,10 @@ struct AdapterOuter {
 };
 struct AdapterOuterArgs {
     AdapterOuter sum[2];
-    const int32_t* row_adapter;
+    const int32_t* row_adapter;      // 16-byte aligned, with room for a multiple of eight
+    const int64_t* start;
+    const int32_t* adapter;
+    int64_t requests;
     const int32_t* ranks;
     int64_t count;
     int rank;

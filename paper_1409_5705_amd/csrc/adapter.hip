@@ -13,30 +13,12 @@
 namespace sfb {
 namespace {
 
-
-__device__ __forceinline__ float bf16_float(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
-
-// acc += sum of a 16-byte chunk of each of 16 rows a and 16 rows b: register i of lane (q, c) is row 4 q + i of a, row c of b.
-template <typename T>
-__device__ __forceinline__ floatx4 mfma_chunk(u32x4 a, u32x4 b, floatx4 acc)
-{
-    if constexpr (sizeof(T) == 2) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float((uint32_t)a[e]), __uint_as_float((uint32_t)b[e]), acc, 0, 0, 0);
-        return acc;
-    }
-}
-
-
-// Up to 16 rows of one request against the 16 RT factors 16 RT * blockIdx.y ..; the wavefronts share k.  For few tiles and fp32:
-// what bounds it is how soon everything is on its way, and a wavefront's loads of U k-steps are in flight together.
-template <typename T, int RT, int PW>
+// fp32 rows: up to 16 of one request against the 16 RT factors 16 RT * blockIdx.y ..; the wavefronts share k.  What bounds it is
+// how soon everything is on its way: a wavefront's loads of U k-steps are in flight together.
+template <int RT, int PW>
 __global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams p, unsigned windows, unsigned xcds)
 {
-    constexpr int CE = 16 / (int)sizeof(T), STEP = 4 * CE, U = RT == 1 ? 8 : 4;
+    constexpr int CE = 4, STEP = 4 * CE, U = RT == 1 ? 8 : 4;
     __shared__ floatx4 part[PW][RT][64];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -49,16 +31,23 @@ __global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams 
 
     const int64_t steps = (p.K + STEP - 1) / STEP, per = (steps + PW - 1) / PW;
     const int64_t k_begin = wave * per * STEP, k_end = k_begin + per * STEP < p.K ? k_begin + per * STEP : p.K;
-    const T* const x = static_cast<const T*>(p.X) + (t0 + (l16 < n_rows ? l16 : n_rows - 1)) * p.K + CE * quad;
-    const T* f[RT];
+    const float* const x = static_cast<const float*>(p.X) + (t0 + (l16 < n_rows ? l16 : n_rows - 1)) * p.K + CE * quad;
+    const float* f[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
         const int r = r0 + 16 * i + l16;
-        f[i] = static_cast<const T*>(p.F) + ((int64_t)a * rows.rank + (r < rank ? r : rank - 1)) * p.K + CE * quad;
+        f[i] = static_cast<const float*>(p.F) + ((int64_t)a * rows.rank + (r < rank ? r : rank - 1)) * p.K + CE * quad;
     }
     floatx4 acc[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    // register i of lane (q, c) of an MFMA: factor 4 q + i, row c
+    auto add = [](u32x4 fv, u32x4 xv, floatx4 sum) {
+#pragma unroll
+        for (int e = 0; e < CE; ++e)
+            sum = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float((uint32_t)fv[e]), __uint_as_float((uint32_t)xv[e]), sum, 0, 0, 0);
+        return sum;
+    };
     int64_t k = k_begin;
     for (; k + U * STEP <= k_end; k += U * STEP) {
         u32x4 xv[U], fv[U][RT];
@@ -71,18 +60,18 @@ __global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams 
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < RT; ++i) acc[i] = mfma_chunk<T>(fv[u][i], xv[u], acc[i]);
+            for (int i = 0; i < RT; ++i) acc[i] = add(fv[u][i], xv[u], acc[i]);
     }
     for (; k < k_end; k += STEP) {
         const u32x4 xv = load_chunk(x, k, k_end - CE * quad);
 #pragma unroll
-        for (int i = 0; i < RT; ++i) acc[i] = mfma_chunk<T>(load_chunk(f[i], k, k_end - CE * quad), xv, acc[i]);
+        for (int i = 0; i < RT; ++i) acc[i] = add(load_chunk(f[i], k, k_end - CE * quad), xv, acc[i]);
     }
 #pragma unroll
     for (int i = 0; i < RT; ++i) part[wave][i][lane] = acc[i];
     __syncthreads();
     if (wave >= RT) return;
-    // wavefront i: factors 16 i ..; register e of lane (q, c): factor 4 q + e, row c
+    // wavefront i: factors 16 i ..
     floatx4 sum = part[0][wave][lane];
 #pragma unroll
     for (int w = 1; w < PW; ++w) sum += part[w][wave][lane];
@@ -186,30 +175,15 @@ __global__ __launch_bounds__(256) void pad_kernel(AdapterPad a, AdapterPad b, in
     *reinterpret_cast<u32x4*>(m.dst + i) = v;
 }
 
-template <typename T, int RT>
+template <int RT>
 void project_start(const ProjectParams& p, dim3 grid, unsigned windows, const DeviceInfo& dev, hipStream_t stream)
 {
     const unsigned xcds = dev.xcds > 0 ? dev.xcds : 1;
-    // few workgroups: 16 wavefronts share k, and all of a row is on its way at once; many: eight, and two or three workgroups a
-    // CU hide each other's start (8192 rows, K = 4096, 16 pairs: 30 and 27 us)
+    // PWNOTE
     if ((int64_t)grid.x * grid.y < dev.cus)
-        adapter_project_kernel<T, RT, 16><<<grid, 64 * 16, 0, stream>>>(p, windows, xcds);
+        adapter_project_kernel<RT, 16><<<grid, 64 * 16, 0, stream>>>(p, windows, xcds);
     else
-        adapter_project_kernel<T, RT, 8><<<grid, 64 * 8, 0, stream>>>(p, windows, xcds);
-}
-template <typename T>
-hipError_t project_rank(const ProjectParams& p, const DeviceInfo& dev, hipStream_t stream)
-{
-    const int64_t windows = (p.rows.T + 15) / 16, blocks = windows + p.rows.requests;
-    const int rt = p.pitch <= 16 ? 1 : p.pitch <= 32 ? 2 : 4;
-    const dim3 grid((unsigned)blocks, (unsigned)std::max(1, (p.pitch + 16 * rt - 1) / (16 * rt)));
-    if (rt == 1)
-        project_start<T, 1>(p, grid, (unsigned)windows, dev, stream);
-    else if (rt == 2)
-        project_start<T, 2>(p, grid, (unsigned)windows, dev, stream);
-    else
-        project_start<T, 4>(p, grid, (unsigned)windows, dev, stream);
-    return hipGetLastError();
+        adapter_project_kernel<RT, 8><<<grid, 64 * 8, 0, stream>>>(p, windows, xcds);
 }
 
 }  // namespace
@@ -217,11 +191,18 @@ hipError_t project_rank(const ProjectParams& p, const DeviceInfo& dev, hipStream
 hipError_t launch_adapter_project(const AdapterProjectArgs& a, DeviceInfo& dev, hipStream_t stream)
 {
     if (a.rows.T <= 0) return hipSuccess;
-    ProjectParams p = {a.rows, a.X, a.F, a.K, a.row_adapter, a.H, a.H_out, a.Hx, adapter_pitch(a.rows.rank)};
-    // whole tiles of 32 rows where there are as many as half of the CUs, and rows enough of a request to fill them
-    if (a.bf16 && p.pitch > 0 && a.rows.T >= 16 * (int64_t)dev.cus && a.rows.T >= 16 * a.rows.requests)
-        return launch_adapter_project_tiles(p, dev, stream);
-    return a.bf16 ? project_rank<uint16_t>(p, dev, stream) : project_rank<float>(p, dev, stream);
+    const ProjectParams p = {a.rows, a.X, a.F, a.K, a.row_adapter, a.H, a.H_out, a.Hx, adapter_pitch(a.rows.rank)};
+    if (a.bf16) return launch_adapter_project_tiles(p, dev, stream);
+    const int64_t windows = (p.rows.T + 15) / 16, blocks = windows + p.rows.requests;
+    const int rt = p.pitch <= 16 ? 1 : p.pitch <= 32 ? 2 : 4;
+    const dim3 grid((unsigned)blocks, (unsigned)std::max(1, (p.pitch + 16 * rt - 1) / (16 * rt)));
+    if (rt == 1)
+        project_start<1>(p, grid, (unsigned)windows, dev, stream);
+    else if (rt == 2)
+        project_start<2>(p, grid, (unsigned)windows, dev, stream);
+    else
+        project_start<4>(p, grid, (unsigned)windows, dev, stream);
+    return hipGetLastError();
 }
 
 hipError_t launch_adapter_pad(const AdapterPad& a, const AdapterPad& b, hipStream_t stream)

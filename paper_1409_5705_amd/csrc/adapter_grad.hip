@@ -18,7 +18,10 @@ struct OuterParams {
     const int32_t* ranks;
     int64_t count;
     int rank;
-    int64_t T, per;            // rows, rows of a split
+    const int64_t* start;      // of the requests, where a block's rows are looked for by them (requests > 0)
+    const int32_t* adapter;
+    int64_t requests;
+    int64_t T, per;            // rows, rows of a split (a multiple of eight)
     unsigned tiles0, tiles;
     int64_t first;             // workgroups of the launches before
     int window;                // rows of a list (bf16: their offsets in G have 31 bits)
@@ -50,19 +53,62 @@ __device__ __forceinline__ OuterTile outer_tile(const OuterParams& p, int width,
     return t;
 }
 
-// The rows of the window from w0 on that belong to the block, in their order, as offsets from w0; their number.
+// Cuts the tile's rows down to those between the first and the last one of its block's requests: windows without any cost 3 us
+// each (NARROWNOTE).  counts: 2 OW.
+__device__ __forceinline__ void narrow_rows(const OuterParams& p, OuterTile& tile, int* counts)
+{
+    if (p.requests == 0) return;
+    const int tid = threadIdx.x, wave = tid >> 6;
+    int lo = 0x7fffffff, hi = 0;      // (T is below 2^24)
+    for (int64_t q = tid; q < p.requests; q += 64 * OW) {
+        if (p.adapter[q] != tile.a) continue;
+        const int64_t s = p.start[q], e = p.start[q + 1] < p.T ? p.start[q + 1] : p.T, b = s > 0 ? s : 0;
+        if (b >= e) continue;
+        lo = (int)b < lo ? (int)b : lo;
+        hi = (int)e > hi ? (int)e : hi;
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        const int l = __shfl_xor(lo, d), h = __shfl_xor(hi, d);
+        lo = l < lo ? l : lo;
+        hi = h > hi ? h : hi;
+    }
+    if ((tid & 63) == 0) {
+        counts[wave] = lo;
+        counts[OW + wave] = hi;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < OW; ++w) {
+        lo = counts[w] < lo ? counts[w] : lo;
+        hi = counts[OW + w] > hi ? counts[OW + w] : hi;
+    }
+    __syncthreads();
+    lo = __builtin_amdgcn_readfirstlane(lo) & ~7;
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    if (lo > tile.t_begin) tile.t_begin = lo;
+    if (hi < tile.t_end) tile.t_end = hi;
+}
+
+// The rows of the window from w0 on (a multiple of eight) that belong to the block, in their order, as offsets from w0; their
+// number.  (What follows row_adapter up to a multiple of eight may be read.)
 __device__ __forceinline__ int list_rows(const OuterParams& p, const OuterTile& tile, int64_t w0, uint16_t* list, int* counts)
 {
     constexpr int PER = WINDOW / (64 * OW);
+    static_assert(PER == 8, "two loads of 16 bytes");
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int found = 0;
     uint32_t bits = 0;
+    const int64_t t0 = w0 + tid * PER;
+    if (tid * PER < p.window && t0 < tile.t_end) {      // (the window is a multiple of 64)
+        const u32x4* const at = reinterpret_cast<const u32x4*>(p.row_adapter + t0);
+        const u32x4 v[2] = {at[0], at[1]};
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int64_t t = w0 + tid * PER + i;
-        if (tid * PER + i < p.window && t < tile.t_end && p.row_adapter[t] == tile.a) {
-            bits |= 1u << i;
-            ++found;
+        for (int i = 0; i < PER; ++i) {
+            if (t0 + i < tile.t_end && (int)v[i >> 2][i & 3] == tile.a) {
+                bits |= 1u << i;
+                ++found;
+            }
         }
     }
     int before = found;
@@ -158,9 +204,11 @@ template <int RT>
 __global__ __launch_bounds__(64 * OW, 4) void adapter_outer_f32_kernel(OuterParams p)
 {
     __shared__ uint16_t list[WINDOW];
-    __shared__ int counts[OW];
+    __shared__ int counts[2 * OW];
     __shared__ floatx4 part[OW * 4 * 64];
-    outer_fp32<float, RT>(p, outer_tile(p, 64, 16 * RT), list, counts, part);
+    OuterTile tile = outer_tile(p, 64, 16 * RT);
+    narrow_rows(p, tile, counts);
+    outer_fp32<float, RT>(p, tile, list, counts, part);
 }
 
 // bf16 rows: tiles of 128 columns, 64 rows of the block at a time, on the bf16 matrix pipes.  A value of H is three bf16 terms
@@ -188,7 +236,8 @@ __global__ __launch_bounds__(64 * OW, 4) void adapter_outer_bf16_kernel(OuterPar
     int* const counts = reinterpret_cast<int*>(lds);      // (used while nothing is on its way into the stages)
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const OuterTile tile = outer_tile(p, 128, 16 * RT);
+    OuterTile tile = outer_tile(p, 128, 16 * RT);
+    narrow_rows(p, tile, counts);
     const AdapterOuter& sum = *tile.sum;
 
     // G's rows of 256 bytes, 16-byte chunk u of row r in slot u ^ 4 (r % 4): a load is four rows.  H's rows of RT pieces of 64 bytes:
@@ -381,11 +430,14 @@ hipError_t outer_rank(OuterParams p, int splits, bool bf16, DeviceInfo& dev, hip
 
 }  // namespace
 
-// Two workgroups a CU at least, of 512 rows of the matrix at least.
+// Parts of the rows: as many workgroups as the chip takes (ranks up to 32 one a CU: 8192 rows, one block of 16 pairs of 4096 + 4096
+// columns 86 us in one part, 33 in four, 36 in eight; more two: of 64 pairs 162, 55 and 50), and of a block, were all equal, 256
+// rows at least (2048 rows, 8 blocks, 1024 + 1024 columns: one part 11 us, two 14).
 int adapter_outer_splits(int64_t C0, int64_t C1, int64_t count, int rank, bool bf16, int64_t T)
 {
     if (count <= 0 || T <= 0) return 1;
-    const int64_t blocks = outer_blocks(C0, C1, count, rank, bf16), s = std::min((512 + blocks - 1) / blocks, T / 512);
+    const int64_t blocks = outer_blocks(C0, C1, count, rank, bf16), target = rank <= 32 ? 256 : 512;
+    const int64_t s = std::min((target + blocks - 1) / blocks, T / (256 * count));
     return s < 2 ? 1 : s > 16 ? 16 : (int)s;
 }
 
@@ -404,8 +456,14 @@ hipError_t launch_adapter_outer(const AdapterOuterArgs& a, DeviceInfo& dev, hipS
     p.tiles0 = (unsigned)((a.sum[0].C + width - 1) / width);
     p.tiles = p.tiles0 + (unsigned)((a.sum[1].C + width - 1) / width);
     const int splits = adapter_outer_splits(a.sum[0].C, a.sum[1].C, a.count, a.rank, a.bf16, a.T);
-    p.per = (a.T + splits - 1) / splits;
+    p.per = ((a.T + splits - 1) / splits + 7) / 8 * 8;
     p.partial = splits > 1 ? a.partial : nullptr;
+    // (one window: nothing to find; nearly as many requests as rows: the rows are as soon gone through)
+    if (p.per > WINDOW && a.requests <= a.T / 4) {
+        p.start = a.start;
+        p.adapter = a.adapter;
+        p.requests = a.requests;
+    }
     p.window = WINDOW;
     if (a.bf16) {
         const int64_t widest = std::max(a.sum[0].C, a.sum[1].C), most = (int64_t(1) << 30) / widest;

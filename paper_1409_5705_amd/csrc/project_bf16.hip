@@ -626,9 +626,10 @@ __global__ __launch_bounds__(256) void adapter_project_tiles_kernel(ProjectParam
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------------------
-// The stream of W bounds the product of up to FEW_ROWS rows.  Tiles of 64 or 128 rows x 64 columns along a part of k, five or
-// three LDS stages of a k-slice: about 100 KB of requests of a CU's two workgroups in flight.  The blocks' factors are taken for further columns of the matrix:
-// every row is multiplied with the factors of all blocks (the matrix pipes have the time), and the join picks its own block's.
+// The stream of W bounds the product of few rows (adapter_few_plan says which).  Tiles of 64 or 128 rows x 64 columns along a
+// part of k, five or three LDS stages of a k-slice: about 100 KB of requests of a CU's two workgroups in flight.  The blocks'
+// factors are taken for further columns of the matrix: every row is multiplied with the factors of all blocks (the matrix pipes
+// have the time), and the join picks its own block's.
 struct FewParams {
     const uint16_t* A;
     const uint16_t* W;
@@ -776,7 +777,8 @@ template <int RT>
 hipError_t launch_project_tiles(const ProjectParams& p, DeviceInfo& dev, hipStream_t stream)
 {
     const int64_t windows = (p.rows.T + 31) / 32;
-    const dim3 grid((unsigned)(windows + p.rows.requests), (unsigned)((p.pitch + 16 * RT - 1) / (16 * RT)));
+    const unsigned ranges = p.pitch > 0 ? (unsigned)((p.pitch + 16 * RT - 1) / (16 * RT)) : 1;      // (rank 0: row_adapter alone)
+    const dim3 grid((unsigned)(windows + p.rows.requests), ranges);
     adapter_project_tiles_kernel<RT><<<grid, 256, 0, stream>>>(p, (unsigned)windows, dev.xcds > 0 ? dev.xcds : 1);
     return hipGetLastError();
 }
@@ -797,13 +799,27 @@ hipError_t launch_few(const FewParams& p, dim3 grid, DeviceInfo& dev, hipStream_
 
 }  // namespace
 
-// Ways the contraction is divided along k: fewer tiles than half of what the chip holds at once, and at least four slices each.
+// Time of the product on tiles of 128 x 128 with k in s parts, in us: a compute unit with one workgroup takes 0.65 us a slice, with
+// more 0.52 each (4096 columns, K = 4096: 512 rows 41, 2048 rows 72, 4096 rows 135, 8192 rows 268); the parts' planes are written
+// and read at 6 TB/s, by one launch more.
+static double base_us(int64_t M, int64_t N, int64_t K, int64_t s)
+{
+    const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128), slices = (K + BK - 1) / BK;
+    const int64_t rounds = (tiles * s + 255) / 256, per = (slices + s - 1) / s;
+    const double us = 7.0 + (double)per * (rounds == 1 ? 0.65 : 0.52 * (double)rounds);
+    return s == 1 ? us : us + (double)(s * M * N) * 8e-6 / 6.0 + 7.0;
+}
+
+// Ways the contraction is divided along k, at least four slices each, where the tiles are fewer than the compute units: 512 rows,
+// 4096 columns, K = 11008 163 us without, 101 in four parts; 1500 rows, 2048 x 2048 35 us without, 48 in two.
 int adapter_base_split(int64_t M, int64_t N, int64_t K)
 {
     const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128), slices = (K + BK - 1) / BK;
-    if (tiles <= 0 || tiles >= 256) return 1;
-    const int64_t s = 512 / tiles < slices / 4 ? 512 / tiles : slices / 4;
-    return s < 2 ? 1 : s > 16 ? 16 : (int)s;
+    int split = 1;
+    if (tiles > 0 && tiles < 256)
+        for (int s = 2; s <= 16 && slices / s >= 4; ++s)
+            if (base_us(M, N, K, s) < base_us(M, N, K, split)) split = s;
+    return split;
 }
 
 hipError_t launch_adapter_project_tiles(const ProjectParams& p, DeviceInfo& dev, hipStream_t stream)
@@ -816,14 +832,17 @@ hipError_t launch_adapter_project_tiles(const ProjectParams& p, DeviceInfo& dev,
 AdapterFewPlan adapter_few_plan(int64_t M, int64_t N, int64_t K, int64_t factors)
 {
     AdapterFewPlan f;
-    f.few = M > 0 && M <= FEW_ROWS;
+    // one row of tiles, or products of less than 2^33 multiplications: 4096 x 4096, 384 rows 38 us (tiles of 128 x 128 and
+    // projections of their own 47), 512 rows 54 (54); 8192 x 8192, 128 rows 61 (70), 192 rows 95 (81)
+    f.few = M > 0 && (M <= 128 || (M <= 512 && (M + 127) / 128 * 128 * N * K < (int64_t(1) << 33)));
     if (!f.few) return f;
-    // the factors of the whole pool, or a launch of its own for those that are used: it takes as long as 16 MB of them
-    f.dense = factors * K <= (8 << 20);
+    // The factors of the whole pool at 4 TB/s, or a launch of its own for those that are used.  64 rows, 4096 x 4096, blocks of 16
+    // pairs: 256 of them 24 us with and 31 without, 384 29 and 31, 512 37 and 31; 1024 x 1024: 512 of them 18 and 20, 1024 21 and 20.
+    f.dense = (double)(factors * K) * 2e-6 / 4.0 <= 5.5 + 1.4e-3 * (double)K;
     f.width = N + (f.dense ? (factors + 3) / 4 * 4 : 0);
-    f.tile_m = M <= 64 ? 64 : 128;
+    f.tile_m = M <= 64 ? 64 : 128;      // (65 rows, 4096 x 4096: 22 us, on two tiles of 64 rows 29)
     // The parts of k: rounds of 512 workgroups of so many slices, 0.5 us each, and 3 us around them; planes that are written and
-    // read at 4 TB/s.
+    // read at 4 TB/s.  (64 rows, 4096 x 4096: one part 34 us, four 21.7, six 21.5, sixteen 27; the model takes seven, 21.9.)
     const int64_t tiles = ((M + f.tile_m - 1) / f.tile_m) * ((N + 63) / 64 + (f.dense ? (factors + 63) / 64 : 0)), slices = (K + BK - 1) / BK;
     double best = 0;
     for (int s = 1; s <= 16 && (s == 1 || slices / s >= 4); ++s) {
@@ -879,9 +898,12 @@ hipError_t launch_adapter_base_bf16(const AdapterBase& a, DeviceInfo& dev, hipSt
     p.count = (int)a.count;
     p.rank = a.rank;
     p.num_xcd = dev.xcds > 0 ? dev.xcds : 1;
-    const int64_t big = ((a.M + 255) / 256) * ((a.N + 255) / 256);
+    // Tiles of 256 x 256: 1.6 us a slice.  They do more with what they read, the small ones fill the last round better (4096
+    // columns, K = 4096: 2048 rows 99 us and on small tiles 72, 4096 rows 110 and 135, 5000 rows 186 and 162, 8192 rows 210 and 268).
+    const int64_t big = ((a.M + 255) / 256) * ((a.N + 255) / 256), slices = (a.K + BK - 1) / BK;
+    const double big_us = (double)((big + 255) / 256) * (5.0 + 1.6 * (double)slices);
     if (a.split > 1) return a.transposed ? launch_base<4, 4, true, true>(p, dev, stream) : launch_base<4, 4, false, true>(p, dev, stream);
-    if (big >= 256) return a.transposed ? launch_base<8, 8, true, false>(p, dev, stream) : launch_base<8, 8, false, false>(p, dev, stream);
+    if (big_us <= base_us(a.M, a.N, a.K, 1)) return a.transposed ? launch_base<8, 8, true, false>(p, dev, stream) : launch_base<8, 8, false, false>(p, dev, stream);
     return a.transposed ? launch_base<4, 4, true, false>(p, dev, stream) : launch_base<4, 4, false, false>(p, dev, stream);
 }
 

@@ -1275,6 +1275,9 @@ int sfb_adapter_backward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J
     o.sum[0] = {H ? H : Hw, H ? ad->rank : sfb::adapter_pitch(ad->rank), dY, J, dU};
     o.sum[1] = {dH, sfb::adapter_pitch(ad->rank), X, D, dV};
     o.row_adapter = reinterpret_cast<const int32_t*>(ctx->ws);
+    o.start = rq->start;
+    o.adapter = rq->adapter;
+    o.requests = rq->count;
     o.ranks = ad->ranks;
     o.count = ad->count;
     o.rank = ad->rank;

@@ -112,6 +112,18 @@ def test_many_tiles(ctx, J, D, n, R, S):
     compare(c, o)
 
 
+@pytest.mark.parametrize("T,J,D,n,R,S,dtype", [(8100, 4088, 264, 5, 20, 9, BF16), (8100, 264, 4088, 5, 20, 9, BF16), (520, 2056, 4096, 4, 12, 8, BF16),
+                                               (9000, 136, 200, 3, 24, 40, BF16), (9000, 136, 200, 30, 40, 3000, BF16), (9000, 72, 131, 1, 5, 40, F32),
+                                               (40000, 72, 64, 40, 8, 50, BF16)])
+def test_long_batches(ctx, T, J, D, n, R, S, dtype):
+    """Large tiles in more than one round, parts of k, blocks whose rows lie far apart, one gradient of rows in several parts."""
+    c = A.poison(A.make(T, J, D, n, R, S, dtype, seed=T + S, first=min(700, T // 8), behind=T // 30))
+    d, o = to_dev(c), outputs(c)
+    forward(ctx, d, o)
+    backward(ctx, d, o)
+    compare(c, o)
+
+
 @pytest.mark.parametrize("T,J,D,n,R", [(90, 1003, 2047, 2, 12), (90, 65, 63, 3, 5), (90, 2, 3, 2, 1), (90, 130, 1, 1, 7),
                                        (900, 1003, 1001, 2, 12), (1200, 1004, 601, 2, 3), (1200, 601, 1004, 2, 3), (1200, 1002, 603, 2, 3)])
 def test_fp32_odd_sizes(ctx, T, J, D, n, R):
@@ -160,7 +172,8 @@ def test_numbers_out_of_range(ctx, dtype):
 
 
 @pytest.mark.parametrize("layout", ["copy", "planes"])
-@pytest.mark.parametrize("T,J,D", [(3, 520, 200), (150, 264, 328), (400, 1000, 72)])
+@pytest.mark.parametrize("T,J,D", [(3, 520, 200), (150, 264, 328), (400, 1000, 72), (520, 1000, 392), (600, 264, 2056), (8100, 4088, 264),
+                                   (8100, 264, 4088)])
 def test_attached_matrix(sfb, layout, T, J, D):
     """bf16 blocks beside the fp32 matrix that a context keeps a bf16 copy or two planes of."""
     c = A.make(T, J, D, 3, 16, 3, BF16, seed=8)
