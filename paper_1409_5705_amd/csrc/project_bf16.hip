@@ -257,13 +257,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
         bool special = false;         // whether the wavefront has met a factor that is not finite
         const int lane = here(threadIdx.x & 63), l16 = lane & 15, quad = lane >> 4, wave = here_scalar(wave0);
         uint64_t left[TBM / 64];      // rows of the tile whose block is still to come
-        int block[TBM / 64];
+        int block[TBM / 64], rank_at[TBM / 64];
 #pragma unroll
         for (int i = 0; i < TBM / 64; ++i) {
             const int64_t m = m0 + 64 * i + lane;
             block[i] = m < p.M ? p.row_adapter[m] : ROW_OUTSIDE;
             left[i] = __builtin_amdgcn_ballot_w64(block[i] >= 0 && block[i] < p.count);
         }
+#pragma unroll
+        for (int i = 0; i < TBM / 64; ++i) rank_at[i] = left[i] >> lane & 1 ? rank_of(p.ranks, p.rank, block[i]) : 0;
         const int pitch = adapter_pitch(p.rank);
         // the H of 16 pairs of all the wavefront's rows (what rows of other blocks hold is not used)
         const uint16_t* hx[TM];
@@ -283,17 +285,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
         for (;;) {
             int of = -1, from = 0, ranks = 0, chunks = 0;
             while (chunks < slots && cur_r < p.rank) {
-                int a = -1;
+                int a = -1, rank = 0;
 #pragma unroll
                 for (int i = 0; i < TBM / 64; ++i)
-                    if (a < 0 && left[i]) a = __builtin_amdgcn_readlane(block[i], (int)__builtin_ctzll(left[i]));
+                    if (a < 0 && left[i]) {
+                        const int at = (int)__builtin_ctzll(left[i]);
+                        a = __builtin_amdgcn_readlane(block[i], at);
+                        rank = __builtin_amdgcn_readlane(rank_at[i], at);
+                    }
                 if (a < 0) {                       // the next 16
                     cur_r += 16;
 #pragma unroll
                     for (int i = 0; i < TBM / 64; ++i) left[i] = all[i];
                     continue;
                 }
-                const int rank = __builtin_amdgcn_readfirstlane(rank_of(p.ranks, p.rank, a));
 #pragma unroll
                 for (int i = 0; i < TBM / 64; ++i) {
                     const uint64_t its = __builtin_amdgcn_ballot_w64(block[i] == a);
