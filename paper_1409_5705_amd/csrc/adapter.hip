@@ -13,9 +13,11 @@
 namespace sfb {
 namespace {
 
+constexpr int PW = 8;      // wavefronts (16, also for few workgroups: 14.5 and 14.2 us for 8 rows, K = 4096)
+
 // fp32 rows: up to 16 of one request against the 16 RT factors 16 RT * blockIdx.y ..; the wavefronts share k.  What bounds it is
 // how soon everything is on its way: a wavefront's loads of U k-steps are in flight together.
-template <int RT, int PW>
+template <int RT>
 __global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams p, unsigned windows, unsigned xcds)
 {
     constexpr int CE = 4, STEP = 4 * CE, U = RT == 1 ? 8 : 4;
@@ -175,17 +177,6 @@ __global__ __launch_bounds__(256) void pad_kernel(AdapterPad a, AdapterPad b, in
     *reinterpret_cast<u32x4*>(m.dst + i) = v;
 }
 
-template <int RT>
-void project_start(const ProjectParams& p, dim3 grid, unsigned windows, const DeviceInfo& dev, hipStream_t stream)
-{
-    const unsigned xcds = dev.xcds > 0 ? dev.xcds : 1;
-    // PWNOTE
-    if ((int64_t)grid.x * grid.y < dev.cus)
-        adapter_project_kernel<RT, 16><<<grid, 64 * 16, 0, stream>>>(p, windows, xcds);
-    else
-        adapter_project_kernel<RT, 8><<<grid, 64 * 8, 0, stream>>>(p, windows, xcds);
-}
-
 }  // namespace
 
 hipError_t launch_adapter_project(const AdapterProjectArgs& a, DeviceInfo& dev, hipStream_t stream)
@@ -193,15 +184,16 @@ hipError_t launch_adapter_project(const AdapterProjectArgs& a, DeviceInfo& dev, 
     if (a.rows.T <= 0) return hipSuccess;
     const ProjectParams p = {a.rows, a.X, a.F, a.K, a.row_adapter, a.H, a.H_out, a.Hx, adapter_pitch(a.rows.rank)};
     if (a.bf16) return launch_adapter_project_tiles(p, dev, stream);
-    const int64_t windows = (p.rows.T + 15) / 16, blocks = windows + p.rows.requests;
-    const int rt = p.pitch <= 16 ? 1 : p.pitch <= 32 ? 2 : 4;
-    const dim3 grid((unsigned)blocks, (unsigned)std::max(1, (p.pitch + 16 * rt - 1) / (16 * rt)));
+    const int64_t windows = (p.rows.T + 15) / 16, tiles = windows + p.rows.requests;
+    const int rt = project_factors(tiles, p.pitch, dev);
+    const dim3 grid((unsigned)tiles, (unsigned)std::max(1, (p.pitch + 16 * rt - 1) / (16 * rt)));
+    const unsigned xcds = dev.xcds > 0 ? dev.xcds : 1;
     if (rt == 1)
-        project_start<1>(p, grid, (unsigned)windows, dev, stream);
+        adapter_project_kernel<1><<<grid, 64 * PW, 0, stream>>>(p, (unsigned)windows, xcds);
     else if (rt == 2)
-        project_start<2>(p, grid, (unsigned)windows, dev, stream);
+        adapter_project_kernel<2><<<grid, 64 * PW, 0, stream>>>(p, (unsigned)windows, xcds);
     else
-        project_start<4>(p, grid, (unsigned)windows, dev, stream);
+        adapter_project_kernel<4><<<grid, 64 * PW, 0, stream>>>(p, (unsigned)windows, xcds);
     return hipGetLastError();
 }
 

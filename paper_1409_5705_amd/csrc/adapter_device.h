@@ -81,6 +81,15 @@ struct ProjectParams {
     int pitch;
 };
 hipError_t launch_adapter_project_tiles(const ProjectParams& p, DeviceInfo& dev, hipStream_t stream);
+// Factors of a workgroup, in MFMA tiles of 16: as few as give every compute unit a
+// workgroup (64 pairs, K = 4096: 700 rows 22 us with 64 a workgroup, 13 with 16; 8192 rows 27, with 16 and 32 31; fp32, 8 rows 37
+// and 14).
+inline int project_factors(int64_t tiles, int pitch, const DeviceInfo& dev)
+{
+    int rt = 1;
+    while (rt < 4 && 16 * rt < pitch && tiles * ((pitch + 16 * rt - 1) / (16 * rt)) > dev.cus) rt *= 2;
+    return rt;
+}
 
 // Two bf16 terms of a value: its upper half as it is and what is left, rounded (together off by at most 2^-17 of the value, and
 // of its sign); one that is not finite as itself twice.

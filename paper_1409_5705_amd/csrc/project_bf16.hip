@@ -16,8 +16,8 @@
 // multiplied with the rows that use it; the others' H counts as zeros there.  A factor that is not finite must not meet those
 // zeros: it counts as zero too, and the rows that use it get its products when they are stored.
 //
-// The matrix pipes bound it where there are tiles enough: 8192 rows, 4096 x 4096 in 219 to 242 us forward (1.2 PFLOP/s) and 193
-// us backward (1.4 PFLOP/s).  What a tile costs besides its k-loop is instructions that are executed once, so their number
+// The matrix pipes bound it where there are tiles enough: 8192 rows, 4096 x 4096 with 16 blocks of 16 pairs in 210 to 227 us
+// either way (1.2 to 1.3 PFLOP/s; the library's product alone 207 to 219, along W's rows 251).  What a tile costs besides its k-loop is instructions that are executed once, so their number
 // counts, and a register that is spilled around them more so (an earlier form with scratch memory and 80 KB of code: 30 us a
 // tile, this one 8).
 #include "adapter_device.h"
@@ -553,13 +553,15 @@ hipError_t launch_base(BaseParams& p, DeviceInfo& dev, hipStream_t stream)
 
 // ---- projections of many rows ---------------------------------------------------------------------------------------------
 // H[t][r] = scale_a sum_k X[t][k] F_a[r][k] on tiles of 32 rows of one request (as adapter_project_kernel divides them) x 16 RT
-// factors.  The stream of X and the factors' way out of the L2 bound it: whole lines straight into LDS, six stages ahead.  (A
-// MFMA operand loaded from memory into its registers takes a line for every lane: 8192 rows, K = 4096, 64 pairs 61 us.)
+// factors.  The stream of X and the factors' way out of the L2 bound it where rows are many: whole lines straight into LDS (8192
+// rows, K = 4096: 16 pairs 22 us, 64 pairs 27 to 29; MFMA operands loaded from memory into their registers, a line for every
+// lane, 27 and 49 to 61).  Where they are few it is what a slice takes, so there are 128 k or more in one (600 rows, 32 pairs:
+// slices of 64 k 15.7 us, of 128 13.2; twice the stages gain nothing).
 // Wavefront w: the k-step w % 2 of every 64 k and the rows 16 (w / 2) .. of the tile.
-template <int RT>
+template <int RT, int KM, int PS>
 __global__ __launch_bounds__(256) void adapter_project_tiles_kernel(ProjectParams p, unsigned windows, unsigned xcds)
 {
-    constexpr int KM = RT == 1 ? 2 : 1, PS = 6, LOADS = KM * (4 + 2 * RT) / 4;      // 64 KM of k a slice; loads of a wavefront
+    constexpr int LOADS = KM * (4 + 2 * RT) / 4;      // 64 KM of k a slice; loads of a wavefront
     static_assert(KM * (4 + 2 * RT) % 4 == 0, "as many loads for every wavefront");
     constexpr uint32_t ROWS_BYTES = 32 * 128, SLAB = ROWS_BYTES + 16 * RT * 128, STAGE_BYTES = KM * SLAB;
     __shared__ u32x4 smem[PS * STAGE_BYTES / 16];
@@ -634,7 +636,8 @@ __global__ __launch_bounds__(256) void adapter_project_tiles_kernel(ProjectParam
 // The stream of W bounds the product of few rows (adapter_few_plan says which).  Tiles of 64 or 128 rows x 64 columns along a
 // part of k, five or three LDS stages of a k-slice: about 100 KB of requests of a CU's two workgroups in flight.  The blocks'
 // factors are taken for further columns of the matrix: every row is multiplied with the factors of all blocks (the matrix pipes
-// have the time), and the join picks its own block's.
+// have the time), and the join picks its own block's.  64 rows, 4096 x 4096, 64 blocks of 16 pairs: 13.4 us and the join's 6.8, of
+// which the matrix takes 7 at the rate of a copy; one row, 8192 x 8192 out of memory 27 to 36 (3.7 to 5 TB/s).
 struct FewParams {
     const uint16_t* A;
     const uint16_t* W;
@@ -784,7 +787,9 @@ hipError_t launch_project_tiles(const ProjectParams& p, DeviceInfo& dev, hipStre
     const int64_t windows = (p.rows.T + 31) / 32;
     const unsigned ranges = p.pitch > 0 ? (unsigned)((p.pitch + 16 * RT - 1) / (16 * RT)) : 1;      // (rank 0: row_adapter alone)
     const dim3 grid((unsigned)(windows + p.rows.requests), ranges);
-    adapter_project_tiles_kernel<RT><<<grid, 256, 0, stream>>>(p, (unsigned)windows, dev.xcds > 0 ? dev.xcds : 1);
+    const unsigned xcds = dev.xcds > 0 ? dev.xcds : 1;
+    constexpr int KM = RT == 1 ? 4 : 2, PS = RT == 2 ? 4 : 3;
+    adapter_project_tiles_kernel<RT, KM, PS><<<grid, 256, 0, stream>>>(p, (unsigned)windows, xcds);
     return hipGetLastError();
 }
 
@@ -829,9 +834,8 @@ int adapter_base_split(int64_t M, int64_t N, int64_t K)
 
 hipError_t launch_adapter_project_tiles(const ProjectParams& p, DeviceInfo& dev, hipStream_t stream)
 {
-    if (p.pitch <= 16) return launch_project_tiles<1>(p, dev, stream);
-    if (p.pitch <= 32) return launch_project_tiles<2>(p, dev, stream);
-    return launch_project_tiles<4>(p, dev, stream);
+    const int rt = project_factors((p.rows.T + 31) / 32 + p.rows.requests, p.pitch, dev);
+    return rt == 1 ? launch_project_tiles<1>(p, dev, stream) : rt == 2 ? launch_project_tiles<2>(p, dev, stream) : launch_project_tiles<4>(p, dev, stream);
 }
 
 AdapterFewPlan adapter_few_plan(int64_t M, int64_t N, int64_t K, int64_t factors)
