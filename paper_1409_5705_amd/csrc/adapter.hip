@@ -80,87 +80,140 @@ __global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams 
     store_projection(p, tile, t0 + l16, l16 < n_rows, r0 + 16 * wave + 4 * quad, sum);
 }
 
-// A thread: four columns of one row of the output.  The row's projections come from H, or (dense) from the planes, which hold
-// the products with the factors of all blocks behind the columns of the output; then the first workgroup of a row stores them.
-template <typename T>
+// A thread: four columns of RW rows of the output, which read their block's factors once where it is the same one.  The rows'
+// projections come from H, or (dense) from the planes, which hold the products with the factors of all blocks behind the
+// columns of the output; then the first workgroup of a row stores them.
+template <typename T, int RW>
 __global__ __launch_bounds__(128) void adapter_join_kernel(AdapterJoinArgs p, int blocks_n, int64_t t0)
 {
-    __shared__ float h_of[256];
-    const int64_t t = t0 + blockIdx.x / blocks_n, n = ((int64_t)(blockIdx.x % blocks_n) * 128 + threadIdx.x) * 4;
+    __shared__ float h_of[RW][256];
+    __shared__ int a_of[RW], rank_at[RW];
+    const int64_t t = t0 + (int64_t)(blockIdx.x / blocks_n) * RW, n = ((int64_t)(blockIdx.x % blocks_n) * 128 + threadIdx.x) * 4;
     const int live = p.N - n < 4 ? p.N - n < 0 ? 0 : (int)(p.N - n) : 4;
-    const int a = p.row_adapter[t];
-    floatx4 v = {0.f, 0.f, 0.f, 0.f};
-    const float* src = p.planes + t * p.width + n;
+    const int64_t plane = p.T * p.width;
+    // a row's block and projections are looked for by threads of its own
+    constexpr int OF_ROW = 128 / RW;
+    const int mine = RW == 1 ? 0 : threadIdx.x / OF_ROW, pitch = adapter_pitch(p.rank);
+    const int64_t row = t + mine;
+    const int of = RW == 1 || row < p.T ? p.row_adapter[row] : ROW_OUTSIDE;
+    floatx4 v[RW];
+    const float* src[RW];
+#pragma unroll
+    for (int j = 0; j < RW; ++j) {
+        v[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+        src[j] = p.planes + (RW == 1 || t + j < p.T ? t + j : p.T - 1) * p.width + n;
+    }
     if (live == 4) {
 #pragma unroll 4
-        for (int s = 0; s < p.split; ++s) v += __builtin_bit_cast(floatx4, load_chunk(src + s * (p.T * p.width)));
+        for (int s = 0; s < p.split; ++s)
+#pragma unroll
+            for (int j = 0; j < RW; ++j) v[j] += __builtin_bit_cast(floatx4, load_chunk(src[j] + s * plane));
     } else {
         for (int s = 0; s < p.split; ++s)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < live) v[e] += src[s * (p.T * p.width) + e];
+            for (int j = 0; j < RW; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < live) v[j][e] += src[j][s * plane + e];
     }
-    if (a == ROW_OUTSIDE) return;
-    const int pitch = adapter_pitch(p.rank);
-    const bool first = blockIdx.x % blocks_n == 0;
-    int rank = 0;
-    if (a >= 0 && a < p.count) {
-        rank = rank_of(p.ranks, p.rank, a);
-        const float scale = p.scale ? p.scale[a] : 1.f;
+    if (RW == 1 && of == ROW_OUTSIDE) return;
+    int its_rank = 0;
+    if (of >= 0 && of < p.count) {
+        its_rank = rank_of(p.ranks, p.rank, of);
+        const float scale = p.scale ? p.scale[of] : 1.f;
         // (all of the row's, those that are not in use too: their number is still on its way)
-        for (int r = threadIdx.x; r < p.rank; r += 128) {
+        for (int r = threadIdx.x % OF_ROW; r < p.rank; r += OF_ROW) {
             float h;
             if (p.dense) {
                 h = 0.f;
-                const float* from = p.planes + t * p.width + p.N + (int64_t)a * p.rank + r;
+                const float* from = p.planes + row * p.width + p.N + (int64_t)of * p.rank + r;
 #pragma unroll 4
-                for (int s = 0; s < p.split; ++s) h += from[s * (p.T * p.width)];
+                for (int s = 0; s < p.split; ++s) h += from[s * plane];
                 h *= scale;
             } else {
-                h = p.H[t * pitch + r];
+                h = p.H[row * pitch + r];
             }
-            h_of[r] = h;
+            h_of[mine][r] = h;
+        }
+        if (RW == 1) __syncthreads();
+    }
+    int a[RW], rank[RW];
+    bool same = RW > 1;
+    if constexpr (RW == 1) {
+        a[0] = of;
+        rank[0] = its_rank;
+    } else {
+        if (threadIdx.x % OF_ROW == 0) {
+            a_of[mine] = of;
+            rank_at[mine] = its_rank;
         }
         __syncthreads();
+#pragma unroll
+        for (int j = 0; j < RW; ++j) {
+            a[j] = __builtin_amdgcn_readfirstlane(a_of[j]);
+            rank[j] = __builtin_amdgcn_readfirstlane(rank_at[j]);
+            same = same && a[j] == a[0];
+        }
     }
-    if (p.dense && first) {
-        for (int r = threadIdx.x; r < pitch; r += 128) {
-            const float h = r < rank ? h_of[r] : 0.f;
-            p.H[t * pitch + r] = h;
-            if (p.H_out && r < p.rank) p.H_out[t * p.rank + r] = h;
+    if (p.dense && blockIdx.x % blocks_n == 0 && of != ROW_OUTSIDE) {
+        for (int r = threadIdx.x % OF_ROW; r < pitch; r += OF_ROW) {
+            const float h = r < its_rank ? h_of[mine][r] : 0.f;
+            p.H[row * pitch + r] = h;
+            if (p.H_out && r < p.rank) p.H_out[row * p.rank + r] = h;
         }
     }
     if (live == 0) return;
-    if (rank > 0) {
-        const T* F = static_cast<const T*>(p.F) + (int64_t)a * p.rank * p.N + n;
-        floatx4 low = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-        for (int r = 0; r < rank; ++r) {
-            const float hr = h_of[r];
-            if constexpr (sizeof(T) == 2) {      // (N % 8 == 0: all four columns)
-                const u32x2 f = *reinterpret_cast<const u32x2*>(F + r * p.N);
+    // the factors that columns n .. n + 3 have for pair r
+    auto factors = [&](const T* F, int r) {
+        floatx4 f;
+        if constexpr (sizeof(T) == 2) {      // (N % 8 == 0: all four columns)
+            const u32x2 w = *reinterpret_cast<const u32x2*>(F + r * p.N);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t w = f[e >> 1];
-                    low[e] = fmaf(hr, __uint_as_float((e & 1) ? w & 0xffff0000u : w << 16), low[e]);
-                }
-            } else {
-                const u32x4 f = load_chunk(F + r * p.N, 0, live);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) low[e] = fmaf(hr, __uint_as_float((uint32_t)f[e]), low[e]);
-            }
+            for (int e = 0; e < 4; ++e) f[e] = __uint_as_float((e & 1) ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+        } else {
+            f = __builtin_bit_cast(floatx4, load_chunk(F + r * p.N, 0, live));
         }
-        v += low;
-    }
-    T* out = static_cast<T*>(p.out) + t * p.N + n;
-    if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<u32x2*>(out) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-    } else if (live == 4) {
-        *reinterpret_cast<u32x4_by_word*>(out) = __builtin_bit_cast(u32x4, v);
+        return f;
+    };
+    floatx4 low[RW];
+#pragma unroll
+    for (int j = 0; j < RW; ++j) low[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (same) {
+        const T* const F = static_cast<const T*>(p.F) + (int64_t)a[0] * p.rank * p.N + n;
+#pragma unroll 8
+        for (int r = 0; r < rank[0]; ++r) {
+            const floatx4 f = factors(F, r);
+#pragma unroll
+            for (int j = 0; j < RW; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) low[j][e] = fmaf(h_of[j][r], f[e], low[j][e]);
+        }
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < live) out[e] = v[e];
+        for (int j = 0; j < RW; ++j) {
+            const T* const F = static_cast<const T*>(p.F) + (int64_t)a[j] * p.rank * p.N + n;
+#pragma unroll 8
+            for (int r = 0; r < rank[j]; ++r) {
+                const floatx4 f = factors(F, r);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) low[j][e] = fmaf(h_of[j][r], f[e], low[j][e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < RW; ++j) {
+        if (a[j] == ROW_OUTSIDE) continue;
+        if (rank[j] > 0) v[j] += low[j];
+        T* const out = static_cast<T*>(p.out) + (t + j) * p.N + n;
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<u32x2*>(out) = u32x2{pack_bf16(v[j][0], v[j][1]), pack_bf16(v[j][2], v[j][3])};
+        } else if (live == 4) {
+            *reinterpret_cast<u32x4_by_word*>(out) = __builtin_bit_cast(u32x4, v[j]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < live) out[e] = v[j][e];
+        }
     }
 }
 
@@ -205,21 +258,29 @@ hipError_t launch_adapter_pad(const AdapterPad& a, const AdapterPad& b, hipStrea
     return hipGetLastError();
 }
 
-hipError_t launch_adapter_join(const AdapterJoinArgs& a, hipStream_t stream)
+template <int RW>
+static hipError_t join_rows(const AdapterJoinArgs& a, hipStream_t stream)
 {
-    if (a.T <= 0) return hipSuccess;
     const int blocks_n = (int)((a.N + 511) / 512);
-    const int64_t rows = std::max<int64_t>(1, MAX_BLOCKS / blocks_n);
-    for (int64_t t0 = 0; t0 < a.T; t0 += rows) {
-        const unsigned blocks = (unsigned)(std::min(rows, a.T - t0) * blocks_n);
+    const int64_t groups = (a.T + RW - 1) / RW, most = std::max<int64_t>(1, MAX_BLOCKS / blocks_n);
+    for (int64_t g = 0; g < groups; g += most) {
+        const unsigned blocks = (unsigned)(std::min(most, groups - g) * blocks_n);
         if (a.bf16)
-            adapter_join_kernel<uint16_t><<<blocks, 128, 0, stream>>>(a, blocks_n, t0);
+            adapter_join_kernel<uint16_t, RW><<<blocks, 128, 0, stream>>>(a, blocks_n, g * RW);
         else
-            adapter_join_kernel<float><<<blocks, 128, 0, stream>>>(a, blocks_n, t0);
+            adapter_join_kernel<float, RW><<<blocks, 128, 0, stream>>>(a, blocks_n, g * RW);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+
+hipError_t launch_adapter_join(const AdapterJoinArgs& a, hipStream_t stream)
+{
+    if (a.T <= 0) return hipSuccess;
+    // Two rows a workgroup where there are eight workgroups and more a compute unit: what the L2s give bounds it then, the factors
+    // most of it (fp32, 64 pairs: 2000 rows, 4096 columns 76 us and with two 47; 300 rows, 1024 columns 11 and 15).
+    return a.T * ((a.N + 511) / 512) < 2048 ? join_rows<1>(a, stream) : join_rows<2>(a, stream);
 }
 
 }  // namespace sfb

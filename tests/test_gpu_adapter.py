@@ -114,7 +114,7 @@ def test_many_tiles(ctx, J, D, n, R, S):
 
 @pytest.mark.parametrize("T,J,D,n,R,S,dtype", [(8100, 4088, 264, 5, 20, 9, BF16), (8100, 264, 4088, 5, 20, 9, BF16), (520, 2056, 4096, 4, 12, 8, BF16),
                                                (9000, 136, 200, 3, 24, 40, BF16), (9000, 136, 200, 30, 40, 3000, BF16), (9000, 72, 131, 1, 5, 40, F32),
-                                               (40000, 72, 64, 40, 8, 50, BF16)])
+                                               (40000, 72, 64, 40, 8, 50, BF16), (385, 4104, 72, 5, 24, 40, BF16), (4601, 136, 200, 3, 24, 700, F32)])
 def test_long_batches(ctx, T, J, D, n, R, S, dtype):
     """Large tiles in more than one round, parts of k, blocks whose rows lie far apart, one gradient of rows in several parts."""
     c = A.poison(A.make(T, J, D, n, R, S, dtype, seed=T + S, first=min(700, T // 8), behind=T // 30))
