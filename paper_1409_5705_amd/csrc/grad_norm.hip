@@ -17,7 +17,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int64_t TARGET = 4096;    // pieces of a whole list, about (1024: a list of 1.7 GB 6 % slower, too few to even out)
 constexpr int64_t MOST = 1 << 23;   // workgroups of a launch
-constexpr int64_t FEW = 8192;       // pieces whose sums every workgroup of the second pass adds up itself
 
 // Tensors of one launch: their description travels as a kernel argument (4 KB of them).
 template <int N, bool CLIP>
@@ -208,6 +207,14 @@ int64_t piece_of(const sfb_tensor* list, int64_t count)
     return per <= 4096 ? 4096 : per <= (1 << 30) ? (per + 4095) / 4096 * 4096 : 1 << 30;
 }
 
+// Whether every workgroup of the second pass adds up the pieces' sums itself, or a launch of its own does: few pieces, or long
+// ones beside which that is nothing.  64 tensors of 65536 elements (1024 pieces) 18 us and 19 with the launch, 4000 of 4096 50 and 44,
+// 8 of 2^24 (4096 pieces) 284 and 287, 12000 of 4096 161 and 119.
+bool sums_itself(const sfb_tensor* list, int64_t count, int64_t pieces)
+{
+    return pieces <= 2048 || (pieces <= 8192 && piece_of(list, count) >= 32768);
+}
+
 // Last piece of a tensor of n elements, and its type.
 uint32_t tail_of(const sfb_tensor& t, int64_t pieces, int64_t piece)
 {
@@ -311,14 +318,14 @@ hipError_t launch_grad_norm(const sfb_tensor* list, int64_t count, const void* t
         });
         if (e != hipSuccess) return e;
     }
-    if (!(clip && pieces > 0 && pieces <= FEW)) grad_norm_final_kernel<<<1, 1024, 0, stream>>>(partial, pieces, norm);
+    if (!(clip && pieces > 0 && sums_itself(list, count, pieces))) grad_norm_final_kernel<<<1, 1024, 0, stream>>>(partial, pieces, norm);
     return hipGetLastError();
 }
 
 hipError_t launch_clip(const sfb_tensor* list, int64_t count, const void* table, const double* partial, double max_norm, float* norm, hipStream_t stream)
 {
     const int64_t pieces = grad_norm_partials(list, count);
-    float* const own = pieces <= FEW ? norm : nullptr;
+    float* const own = sums_itself(list, count, pieces) ? norm : nullptr;
     if (table && pieces > 0 && pieces <= MOST) {
         const TableParams p = table_params(list, count, table);
         clip_kernel<TableParams><<<(unsigned)pieces, 256, 0, stream>>>(p, partial, pieces, max_norm, own, own != nullptr);

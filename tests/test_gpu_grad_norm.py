@@ -53,6 +53,7 @@ LISTS = [
     ([3 + 17 * k for k in range(300)], lambda k: k % 2),
     ([5_000_003, 17, 1_234_567, 64], lambda k: 0),
     ([1] * 1500, lambda k: 0),
+    ([4097] * 1100, lambda k: 0),
 ]
 
 
