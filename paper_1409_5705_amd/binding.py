@@ -265,6 +265,7 @@ class TensorList:
         if need < 0:
             raise SfbError(int(need), "sfb_grad_norm_workspace_bytes")
         self.workspace_bytes = int(need)
+        self.disjoint = None             # whether they can be clipped (found by the first call that does)
         self.table, self.table_ptr = None, None
         if self.count > 160:             # more than a launch takes as its arguments: described in device memory
             host = torch.zeros(int(lib().sfb_tensor_table_bytes(self.count)), dtype=torch.uint8)
@@ -273,6 +274,30 @@ class TensorList:
                 raise SfbError(rc, "sfb_tensor_table_fill")
             self.table = host.to(self.device)        # (waits for the copy: any stream may use it)
             self.table_ptr = self.table.data_ptr()
+
+    def can_clip(self):
+        """Whether no tensor that clipping writes overlaps another one of the list."""
+        if self.disjoint is None:
+            size = {SFB_F32: 4, SFB_BF16: 2}
+            spans = []
+            for k in range(self.count):
+                item = self.items[k]
+                if item.n:
+                    bytes_ = item.n * size[item.dtype]
+                    spans.append((item.dst, item.dst + bytes_, True))
+                    if item.src != item.dst:
+                        spans.append((item.src, item.src + bytes_, False))
+            spans.sort()
+            end = end_written = 0
+            self.disjoint = True
+            for first, last, written in spans:
+                if first < (end if written else end_written):
+                    self.disjoint = False
+                    break
+                end = max(end, last)
+                if written:
+                    end_written = max(end_written, last)
+        return self.disjoint
 
 
 class Context:
@@ -610,7 +635,10 @@ class Context:
         [0, n): none).  start int64 [S + 1] and adapter int32 [S] on the device; rows of no request stay as they are."""
         J, D, T, n, R, dtype, ad, rq, Wp, Xp = self._adapters(W, X, start, adapter, U, V, ranks, scale)
         self._adapter_workspace("sfb_adapter_forward_workspace_bytes", J, D, T, ad)
-        rc = lib().sfb_adapter_forward(self._h, Wp, _dtype_code(W), J, D, Xp, T, ad, rq, self._at(Y, "Y", dtype, (T, J)),
+        Yp = self._at(Y, "Y", dtype, (T, J))
+        if Yp == Xp and T:
+            raise ValueError("Y must not be X: the call reads X while it writes")
+        rc = lib().sfb_adapter_forward(self._h, Wp, _dtype_code(W), J, D, Xp, T, ad, rq, Yp,
                                        None if H is None else self._at(H, "H", torch.float32, (T, R)))
         self._check(rc, "sfb_adapter_forward")
 
@@ -620,9 +648,12 @@ class Context:
         J, D, T, n, R, dtype, ad, rq, Wp, Xp = self._adapters(W, X, start, adapter, U, V, ranks, scale)
         self._adapter_workspace("sfb_adapter_backward_workspace_bytes", J, D, T, ad)
         at, f32 = self._at, torch.float32
-        rc = lib().sfb_adapter_backward(self._h, Wp, _dtype_code(W), J, D, Xp, at(dY, "dY", dtype, (T, J)), T, ad, rq,
+        dYp, dXp = at(dY, "dY", dtype, (T, J)), None if dX is None else at(dX, "dX", dtype, (T, D))
+        if T and (dXp == dYp or dXp == Xp):
+            raise ValueError("dX must be neither dY nor X: the call reads them while it writes")
+        rc = lib().sfb_adapter_backward(self._h, Wp, _dtype_code(W), J, D, Xp, dYp, T, ad, rq,
                                         None if H is None else at(H, "H", f32, (T, R)),
-                                        None if dX is None else at(dX, "dX", dtype, (T, D)),
+                                        dXp,
                                         None if dU is None else at(dU, "dU", f32, (n, R, J)),
                                         None if dV is None else at(dV, "dV", f32, (n, R, D)))
         self._check(rc, "sfb_adapter_backward")
@@ -642,6 +673,8 @@ class Context:
     def sfb_clip_grads(self, tensors: TensorList, max_norm, norm):
         """Enqueues norm[0] and dst = src * min(1, max_norm / norm) for every tensor of the list."""
         p = self._list(tensors, norm)
+        if not tensors.can_clip():
+            raise ValueError("tensors that are clipped must not overlap (one of them listed twice?)")
         self._check(lib().sfb_clip_grads(self._h, tensors.items, tensors.count, tensors.table_ptr, float(max_norm), p), "sfb_clip_grads")
 
     def sfb_prox_rows(self, W, mode=SFB_PROX_PROJECT):

@@ -329,6 +329,19 @@ def test_wrong_arguments(sfb, ctx):
     assert bool((o["Y"] == o["Y"].new_full((1,), SENTINEL)).all())
 
 
+def test_output_over_input(ctx):
+    c = A.make(20, 64, 64, 2, 8, 3, BF16, seed=1)
+    d, o = to_dev(c), outputs(c)
+    with pytest.raises(ValueError):
+        forward(ctx, d, dict(o, Y=d["X"]))
+    for key in ("dY", "X"):
+        with pytest.raises(ValueError):
+            backward(ctx, d, dict(o, dX=d[key]))
+    torch.cuda.synchronize()
+    for key in ("X", "dY"):
+        assert torch.equal(d[key].cpu(), c[key])
+
+
 def test_large_offsets(ctx):
     """Buffers of more than 2^31 elements: the last rows of X and the last blocks of the pool."""
     T, J, D, n, R = 70000, 64, 32768, 1100, 64

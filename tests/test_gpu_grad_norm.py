@@ -209,3 +209,21 @@ def test_wrong_arguments(sfb, ctx):
     with pytest.raises((TypeError, ValueError)):
         ctx.sfb_grad_norm(sfb.TensorList([a]), norm.double())
     assert bool((a == 1).all())
+
+
+def test_overlapping_tensors(sfb, ctx):
+    """A tensor listed twice counts twice in the norm, and is not clipped: whose scaling is to come first?"""
+    a, b = tensors([1000, 500], seed=8, bf16=lambda k: False)
+    norm = torch.zeros(1, device="cuda:0")
+    ctx.sfb_grad_norm(sfb.TensorList([a, b, a]), norm)
+    assert abs(norm.item() - norm64([a, b, a])) <= 2.0 ** -23 * norm64([a, b, a])
+    keep = [a.clone(), b.clone()]
+    whole = torch.zeros(2000, device="cuda:0")
+    for src, dst in (([a, b, a], None), ([a, a[10:20]], None), ([b, a], [a[:500], torch.empty_like(a)]),
+                     ([a, a], [whole[:1000], whole[999:1999]])):
+        with pytest.raises(ValueError):
+            ctx.sfb_clip_grads(sfb.TensorList(src, dst), 1.0, norm)
+    assert torch.equal(a, keep[0]) and torch.equal(b, keep[1]) and not bool(whole.any())
+    ctx.sfb_clip_grads(sfb.TensorList([a, a], [whole[:1000], whole[1000:]]), 1.0, norm)          # read twice: two results
+    assert torch.equal(whole[:1000], whole[1000:])
+    check_clipped([a], [whole[:1000]], 1.0 / norm64([a, a]))
