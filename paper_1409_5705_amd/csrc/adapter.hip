@@ -83,7 +83,8 @@ __global__ __launch_bounds__(64 * PW) void adapter_project_kernel(ProjectParams 
 // A thread: four columns of RW rows of the output, which read their block's factors once where it is the same one.  The rows'
 // projections come from H, or (dense) from the planes, which hold the products with the factors of all blocks behind the
 // columns of the output; then the first workgroup of a row stores them.
-template <typename T, int RW>
+// PRE: so many factors of the row's block are on their way before its projections are known.
+template <typename T, int RW, int PRE>
 __global__ __launch_bounds__(128) void adapter_join_kernel(AdapterJoinArgs p, int blocks_n, int64_t t0)
 {
     __shared__ float h_of[RW][256];
@@ -117,8 +118,25 @@ __global__ __launch_bounds__(128) void adapter_join_kernel(AdapterJoinArgs p, in
                     if (e < live) v[j][e] += src[j][s * plane + e];
     }
     if (RW == 1 && of == ROW_OUTSIDE) return;
+    // the factors that columns n .. n + 3 have for pair r
+    auto factors = [&](const T* F, int r) {
+        floatx4 f;
+        if constexpr (sizeof(T) == 2) {      // (N % 8 == 0: all four columns)
+            const u32x2 w = *reinterpret_cast<const u32x2*>(F + r * p.N);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] = __uint_as_float((e & 1) ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+        } else {
+            f = __builtin_bit_cast(floatx4, load_chunk(F + r * p.N, 0, live));
+        }
+        return f;
+    };
+    static_assert(PRE == 0 || (RW == 1 && sizeof(T) == 2), "one row, four whole columns a thread");
+    floatx4 pre[PRE > 0 ? PRE : 1];
     int its_rank = 0;
     if (of >= 0 && of < p.count) {
+#pragma unroll
+        for (int r = 0; r < PRE; ++r)
+            pre[r] = factors(static_cast<const T*>(p.F) + (int64_t)of * p.rank * p.N + (live == 4 ? n : 0), r < p.rank ? r : p.rank - 1);
         its_rank = rank_of(p.ranks, p.rank, of);
         const float scale = p.scale ? p.scale[of] : 1.f;
         // (all of the row's, those that are not in use too: their number is still on its way)
@@ -163,18 +181,6 @@ __global__ __launch_bounds__(128) void adapter_join_kernel(AdapterJoinArgs p, in
         }
     }
     if (live == 0) return;
-    // the factors that columns n .. n + 3 have for pair r
-    auto factors = [&](const T* F, int r) {
-        floatx4 f;
-        if constexpr (sizeof(T) == 2) {      // (N % 8 == 0: all four columns)
-            const u32x2 w = *reinterpret_cast<const u32x2*>(F + r * p.N);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) f[e] = __uint_as_float((e & 1) ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
-        } else {
-            f = __builtin_bit_cast(floatx4, load_chunk(F + r * p.N, 0, live));
-        }
-        return f;
-    };
     floatx4 low[RW];
 #pragma unroll
     for (int j = 0; j < RW; ++j) low[j] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -192,8 +198,14 @@ __global__ __launch_bounds__(128) void adapter_join_kernel(AdapterJoinArgs p, in
 #pragma unroll
         for (int j = 0; j < RW; ++j) {
             const T* const F = static_cast<const T*>(p.F) + (int64_t)a[j] * p.rank * p.N + n;
+#pragma unroll
+            for (int r = 0; r < PRE; ++r) {
+                const float h = h_of[j][r];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) low[j][e] = r < rank[j] ? fmaf(h, pre[r][e], low[j][e]) : low[j][e];
+            }
 #pragma unroll 8
-            for (int r = 0; r < rank[j]; ++r) {
+            for (int r = PRE; r < rank[j]; ++r) {
                 const floatx4 f = factors(F, r);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) low[j][e] = fmaf(h_of[j][r], f[e], low[j][e]);
@@ -258,17 +270,14 @@ hipError_t launch_adapter_pad(const AdapterPad& a, const AdapterPad& b, hipStrea
     return hipGetLastError();
 }
 
-template <int RW>
+template <typename T, int RW, int PRE>
 static hipError_t join_rows(const AdapterJoinArgs& a, hipStream_t stream)
 {
     const int blocks_n = (int)((a.N + 511) / 512);
     const int64_t groups = (a.T + RW - 1) / RW, most = std::max<int64_t>(1, MAX_BLOCKS / blocks_n);
     for (int64_t g = 0; g < groups; g += most) {
         const unsigned blocks = (unsigned)(std::min(most, groups - g) * blocks_n);
-        if (a.bf16)
-            adapter_join_kernel<uint16_t, RW><<<blocks, 128, 0, stream>>>(a, blocks_n, g * RW);
-        else
-            adapter_join_kernel<float, RW><<<blocks, 128, 0, stream>>>(a, blocks_n, g * RW);
+        adapter_join_kernel<T, RW, PRE><<<blocks, 128, 0, stream>>>(a, blocks_n, g * RW);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -280,7 +289,12 @@ hipError_t launch_adapter_join(const AdapterJoinArgs& a, hipStream_t stream)
     if (a.T <= 0) return hipSuccess;
     // Two rows a workgroup where there are eight workgroups and more a compute unit: what the L2s give bounds it then, the factors
     // most of it (fp32, 64 pairs: 2000 rows, 4096 columns 76 us and with two 47; 300 rows, 1024 columns 11 and 15).
-    return a.T * ((a.N + 511) / 512) < 2048 ? join_rows<1>(a, stream) : join_rows<2>(a, stream);
+    const bool two = a.T * ((a.N + 511) / 512) >= 2048;
+    if (!a.bf16) return two ? join_rows<float, 2, 0>(a, stream) : join_rows<float, 1, 0>(a, stream);
+    if (two) return join_rows<uint16_t, 2, 0>(a, stream);
+    // (a call of 64 requests, 4096 x 4096, blocks of 16 pairs: 18.4 us, with 16 factors ahead 17.4, with eight 18.6; of 200 rows, 1000 x 520,
+    // blocks of eight pairs: 22.3, with 16 ahead 22.5)
+    return a.rank > 8 ? join_rows<uint16_t, 1, 16>(a, stream) : join_rows<uint16_t, 1, 0>(a, stream);
 }
 
 }  // namespace sfb
