@@ -636,7 +636,7 @@ __global__ __launch_bounds__(256) void adapter_project_tiles_kernel(ProjectParam
 // The stream of W bounds the product of few rows (adapter_few_plan says which).  Tiles of 64 or 128 rows x 64 columns along a
 // part of k, five or three LDS stages of a k-slice: about 100 KB of requests of a CU's two workgroups in flight.  The blocks'
 // factors are taken for further columns of the matrix: every row is multiplied with the factors of all blocks (the matrix pipes
-// have the time), and the join picks its own block's.  64 rows, 4096 x 4096, 64 blocks of 16 pairs: 13.4 us and the join's 6.8, of
+// have the time), and the join picks its own block's.  64 rows, 4096 x 4096, 32 blocks of 16 pairs: 12.8 us and the join's 5.2, of
 // which the matrix takes 7 at the rate of a copy; one row, 8192 x 8192 out of memory 27 to 36 (3.7 to 5 TB/s).
 struct FewParams {
     const uint16_t* A;
