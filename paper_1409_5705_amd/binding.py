@@ -301,7 +301,8 @@ class TensorList:
 
 
 class Context:
-    """One sfb_ctx bound to a device and a stream; owns a torch workspace tensor."""
+    """One sfb_ctx bound to a device and a stream; owns a torch workspace tensor.  Graphs that captured its calls work in memory
+    that it holds: keep it for as long as they are replayed."""
 
     def __init__(self, device=0, stream=None):
         self._h = ctypes.c_void_p()
@@ -314,6 +315,7 @@ class Context:
             raise SfbError(rc, "sfb_create")
         self._ws = None
         self._captured, self._retired = False, []      # workspaces that captured graphs may still work in
+        self._tables = {}                              # and tables of lists that they read (by their ids)
         self._index = self.device.index or 0
         self._ad, self._rq, self._needs = sfb_adapters(), sfb_requests(), {}
         self._shadow = None          # (W tensor, buffer tensor)
@@ -588,11 +590,17 @@ class Context:
             raise ValueError("%s must be on %s, got %s" % (name, self.device, t.device))
         return p
 
+    def _capturing(self):
+        """Whether the context's stream is being captured into a graph."""
+        if torch._C._cuda_getCurrentStream(self._index)[0] == self.stream.stream_id and torch.cuda.current_device() == self._index:
+            return torch._C._cuda_isCurrentStreamCapturing()
+        with torch.cuda.stream(self.stream):
+            return torch._C._cuda_isCurrentStreamCapturing()
+
     def _stream_workspace(self, need):
         """Room for `need` bytes, allocated on the context's stream.  What a captured graph works in stays allocated when the
         workspace grows: the graph replays on the old one."""
-        capturing = torch._C._cuda_isCurrentStreamCapturing()
-        self._captured = self._captured or capturing
+        self._captured = self._captured or self._capturing()
         if self._ws is None or need > self._ws.numel():
             if self._ws is not None and not self._captured:
                 self._ws.record_stream(self.stream)
@@ -663,6 +671,12 @@ class Context:
         if tensors.device is not None and tensors.device != self.device:
             raise ValueError("the tensors must be on %s, got %s" % (self.device, tensors.device))
         self._stream_workspace(tensors.workspace_bytes)
+        if tensors.table is not None:
+            # the list may be gone before the kernels are, and its table belongs to the stream that was current when it was made
+            if self._capturing():
+                self._tables[id(tensors.table)] = tensors.table          # (every replay reads it)
+            else:
+                tensors.table.record_stream(self.stream)
         return self._at(norm, "norm", torch.float32, (1,))
 
     def sfb_grad_norm(self, tensors: TensorList, norm):

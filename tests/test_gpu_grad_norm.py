@@ -227,3 +227,57 @@ def test_overlapping_tensors(sfb, ctx):
     ctx.sfb_clip_grads(sfb.TensorList([a, a], [whole[:1000], whole[1000:]]), 1.0, norm)          # read twice: two results
     assert torch.equal(whole[:1000], whole[1000:])
     check_clipped([a], [whole[:1000]], 1.0 / norm64([a, a]))
+
+
+def test_lists_replaced_on_another_stream(sfb):
+    """Lists of more tensors than a launch takes as its arguments, each made on the current stream for one call on a context of
+    another one and gone before the call's kernels are: every call sees its own tensors."""
+    side = torch.cuda.Stream()
+    own = sfb.Context(0, stream=side)
+    count, rounds = 200, 24
+    flat = [torch.randn(count * 5000, generator=torch.Generator(device="cuda:0").manual_seed(k), device="cuda:0") for k in range(rounds)]
+    before = [f.clone() for f in flat]
+    busy = torch.randn(1 << 26, device="cuda:0")
+    norms = [torch.zeros(1, device="cuda:0") for _ in range(2 * rounds)]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(8):                   # work in front of the calls, so that the lists are gone first
+            busy.mul_(0.5)
+    for k, f in enumerate(flat):
+        own.sfb_grad_norm(sfb.TensorList(f.split(5000)), norms[2 * k])
+        own.sfb_clip_grads(sfb.TensorList(f.split(5000)), 1.0 + k, norms[2 * k + 1])
+    torch.cuda.synchronize()
+    for k, f in enumerate(flat):
+        want = norm64([before[k]])
+        for n in norms[2 * k:2 * k + 2]:
+            assert abs(n.item() - want) <= 2.0 ** -24 * want * 1.001
+        check_clipped([before[k]], [f], (1.0 + k) / want)
+    own.close()
+
+
+def test_captured_list_is_gone(sfb):
+    """A graph of a call with a list that nobody else keeps, replayed after other lists have been made and used."""
+    side = torch.cuda.Stream()
+    own = sfb.Context(0, stream=side)
+    flat = torch.zeros(200 * 300, device="cuda:0")
+    other = torch.randn(200 * 300, device="cuda:0")
+    norm, n2 = torch.zeros(1, device="cuda:0"), torch.zeros(1, device="cuda:0")
+    own.sfb_clip_grads(sfb.TensorList(other.split(300)), 1e9, n2)
+    torch.cuda.synchronize()
+    lst = sfb.TensorList(flat.split(300))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        own.sfb_clip_grads(lst, 1.0, norm)
+    del lst
+    for k in range(3):
+        for _ in range(4):
+            own.sfb_clip_grads(sfb.TensorList(other.split(300)), 1e9, n2)
+        src = torch.randn(200 * 300, generator=torch.Generator(device="cuda:0").manual_seed(k), device="cuda:0")
+        flat.copy_(src)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = norm64([src])
+        assert abs(norm.item() - want) <= 2.0 ** -24 * want * 1.001
+        check_clipped([src], [flat], 1.0 / want)
+    own.close()
