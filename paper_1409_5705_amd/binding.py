@@ -314,7 +314,7 @@ class Context:
         if rc != SFB_OK:
             raise SfbError(rc, "sfb_create")
         self._ws = None
-        self._captured, self._retired = False, []      # workspaces that captured graphs may still work in
+        self._captured, self._retired = False, []      # whether a graph works in _ws; the workspaces before it that graphs work in
         self._tables = {}                              # and tables of lists that they read (by their ids)
         self._index = self.device.index or 0
         self._ad, self._rq, self._needs = sfb_adapters(), sfb_requests(), {}
@@ -404,14 +404,18 @@ class Context:
 
     def sfb_set_workspace(self, tensor):
         """Use `tensor` (uint8, device) as scratch; None clears it."""
-        if self._captured and self._ws is not None and self._ws is not tensor:
-            self._retired.append(self._ws)
         if tensor is None:
             self._check(lib().sfb_set_workspace(self._h, None, 0), "sfb_set_workspace")
         else:
             self._check(lib().sfb_set_workspace(self._h, tensor.data_ptr(), tensor.numel() * tensor.element_size()),
                         "sfb_set_workspace")
-        self._ws = tensor
+        old, self._ws = self._ws, tensor
+        if old is not None and old is not tensor:
+            if self._captured:
+                self._retired.append(old)
+                self._captured = False
+            else:
+                old.record_stream(self.stream)       # (it may belong to another one)
 
     def sfb_apply_workspace_bytes(self, J, D, N, sf_dtype) -> int:
         n = lib().sfb_apply_workspace_bytes(J, D, N, sf_dtype)
@@ -419,19 +423,27 @@ class Context:
             raise SfbError(int(n), "sfb_apply_workspace_bytes")
         return int(n)
 
+    def _capturing(self):
+        """Whether the context's stream is being captured into a graph."""
+        if torch._C._cuda_getCurrentStream(self._index)[0] == self.stream.stream_id and torch._C._cuda_getDevice() == self._index:
+            return torch._C._cuda_isCurrentStreamCapturing()
+        with torch.cuda.stream(self.stream):
+            return torch._C._cuda_isCurrentStreamCapturing()
+
     def _grow_workspace(self, need):
-        have = 0 if self._ws is None else self._ws.numel()
-        if need > have:
-            self.sfb_set_workspace(torch.empty(need, dtype=torch.uint8, device=self.device))
+        """Room for `need` bytes, allocated on the context's stream; every call that takes a workspace comes here.  What a captured
+        graph works in stays allocated when the workspace is replaced: the graph replays on the old one."""
+        if need > (0 if self._ws is None else self._ws.numel()):
+            with torch.cuda.stream(self.stream):
+                self.sfb_set_workspace(torch.empty(need, dtype=torch.uint8, device=self.device))
+        self._captured = self._captured or self._capturing()
 
     def _ensure_workspace(self, model, J, D, batch, W=None):
         need = self.sfb_workspace_bytes(model, J, D, batch)
         if (model == SFB_MLR and batch.in_dtype == SFB_BF16 and self._shadow is not None and W is not None
                 and self._shadow[0].data_ptr() == W.data_ptr() and tuple(self._shadow[0].shape) == (J, D)):
             need -= lib().sfb_shadow_bytes(J, D)
-        have = 0 if self._ws is None else self._ws.numel()
-        if need > have:
-            self.sfb_set_workspace(torch.empty(need, dtype=torch.uint8, device=self.device))
+        self._grow_workspace(need)
 
     # -- the calls of the path --------------------------------------------
     def sfb_compute_sf(self, model, W, X, Y=None, sim=None, U=None, V=None, n_active=None,
@@ -590,23 +602,6 @@ class Context:
             raise ValueError("%s must be on %s, got %s" % (name, self.device, t.device))
         return p
 
-    def _capturing(self):
-        """Whether the context's stream is being captured into a graph."""
-        if torch._C._cuda_getCurrentStream(self._index)[0] == self.stream.stream_id and torch.cuda.current_device() == self._index:
-            return torch._C._cuda_isCurrentStreamCapturing()
-        with torch.cuda.stream(self.stream):
-            return torch._C._cuda_isCurrentStreamCapturing()
-
-    def _stream_workspace(self, need):
-        """Room for `need` bytes, allocated on the context's stream.  What a captured graph works in stays allocated when the
-        workspace grows: the graph replays on the old one."""
-        self._captured = self._captured or self._capturing()
-        if self._ws is None or need > self._ws.numel():
-            if self._ws is not None and not self._captured:
-                self._ws.record_stream(self.stream)
-            with torch.cuda.stream(self.stream):
-                self.sfb_set_workspace(torch.empty(need, dtype=torch.uint8, device=self.device))
-
     def _adapter_workspace(self, query, J, D, T, ad):
         key = (query, J, D, T, ad.count, ad.rank, ad.dtype)
         need = self._needs.get(key)
@@ -617,7 +612,7 @@ class Context:
             if len(self._needs) > 1000:
                 self._needs.clear()
             self._needs[key] = need
-        self._stream_workspace(need)
+        self._grow_workspace(need)
 
     def _adapters(self, W, X, start, adapter, U, V, ranks, scale):
         J, D = W.shape
@@ -670,7 +665,7 @@ class Context:
     def _list(self, tensors, norm):
         if tensors.device is not None and tensors.device != self.device:
             raise ValueError("the tensors must be on %s, got %s" % (self.device, tensors.device))
-        self._stream_workspace(tensors.workspace_bytes)
+        self._grow_workspace(tensors.workspace_bytes)
         if tensors.table is not None:
             # the list may be gone before the kernels are, and its table belongs to the stream that was current when it was made
             if self._capturing():

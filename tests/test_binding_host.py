@@ -37,7 +37,7 @@ class Machine:
     def __init__(self):
         self.default, self.side = Stream(1), Stream(2)
         self.current, self.captured = self.default, None
-        self.bytes = {"sfb_apply_workspace_bytes": 100, "sfb_adapter_forward_workspace_bytes": 100}
+        self.bytes = {"sfb_apply_workspace_bytes": 100, "sfb_workspace_bytes": 100, "sfb_adapter_forward_workspace_bytes": 100}
 
     def __getattr__(self, name):          # the library: every call succeeds, every query is answered from `bytes`
         if not name.startswith("sfb_"):
@@ -66,7 +66,7 @@ def machine(monkeypatch):
     monkeypatch.setattr(binding.Context, "_at", lambda self, t, *args: id(t))
     monkeypatch.setattr(torch, "empty", lambda size, **kw: Memory(size, m.current))
     monkeypatch.setattr(torch.cuda, "stream", m.on)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
     monkeypatch.setattr(torch._C, "_cuda_getCurrentStream", lambda index: (m.current.stream_id, index, 1), raising=False)
     monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: m.current is m.captured, raising=False)
     return m
@@ -109,6 +109,66 @@ def test_table_of_a_captured_call(machine, inside):
         clip(ctx, table)
     clip(ctx, other)
     assert holds(ctx, table) and not holds(ctx, other)
+
+
+def forward(ctx, rows=2):
+    X, W, Y = torch.zeros(rows, 8), torch.zeros(8, 8), torch.zeros(rows, 8)
+    ctx.sfb_adapter_forward(W, X, torch.zeros(2), torch.zeros(1), torch.zeros(1, 1, 8), torch.zeros(1, 1, 8), Y)
+
+
+def apply(ctx, rows=2):
+    ctx.sfb_apply(torch.zeros(8, 8), torch.zeros(rows, 8), torch.zeros(rows, 8), 1.0)
+
+
+def compute(ctx, rows=2):
+    ctx.sfb_compute_sf(sfb.SFB_SC, torch.zeros(8, 8), torch.zeros(rows, 8), U=torch.zeros(rows, 8), V=torch.zeros(rows, 8))
+
+
+CALLS = {apply: "sfb_apply_workspace_bytes", compute: "sfb_workspace_bytes", forward: "sfb_adapter_forward_workspace_bytes"}
+
+
+@pytest.mark.parametrize("captured", CALLS)
+@pytest.mark.parametrize("grows", CALLS)
+@pytest.mark.parametrize("inside", [True, False])
+def test_workspace_of_a_captured_call(machine, captured, grows, inside):
+    """Whichever call was captured and whichever one needs more room later: what the graph works in stays, and only that."""
+    ctx = sfb.Context(0, stream=machine.side)
+    machine.bytes.update(dict.fromkeys(CALLS.values(), 50))
+    captured(ctx)
+    with machine.capture(machine.side), contextlib.nullcontext() if inside else machine.on(machine.default):
+        captured(ctx)                       # (no growth)
+    first = ctx._ws
+    machine.bytes.update(dict.fromkeys(CALLS.values(), 500))
+    grows(ctx, 3)
+    second = ctx._ws
+    assert second is not first and holds(ctx, first)
+    machine.bytes.update(dict.fromkeys(CALLS.values(), 1000))
+    grows(ctx, 4)
+    assert holds(ctx, first) and not holds(ctx, second)
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_workspace_that_is_replaced(machine, call):
+    """It belongs to the context's stream, or the allocator is told that this stream has used it."""
+    ctx = sfb.Context(0, stream=machine.side)
+    call(ctx)
+    first = ctx._ws
+    machine.bytes[CALLS[call]] = 1000
+    call(ctx, 3)
+    assert ctx._ws is not first and (first.stream is machine.side or machine.side in first.used_on)
+    ctx.sfb_set_workspace(Memory(5000, machine.default))
+    theirs = ctx._ws
+    ctx.sfb_set_workspace(None)
+    assert machine.side in theirs.used_on
+
+
+def test_workspace_that_a_captured_call_brings(machine):
+    ctx = sfb.Context(0, stream=machine.side)
+    with machine.capture(machine.side):
+        apply(ctx)
+    first = ctx._ws
+    ctx.sfb_set_workspace(Memory(5000, machine.side))
+    assert holds(ctx, first)
 
 
 def holds(ctx, memory):

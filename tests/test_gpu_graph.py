@@ -172,3 +172,49 @@ def test_apply_static_replays_from_a_graph(sfb, dtype):
         junk = torch.randn(1 << 20, device="cuda:0").sum().item()
         assert np.isfinite(junk)
     ctx.close()
+
+
+def test_workspace_grows_after_a_captured_step(sfb):
+    """A graph of the older calls, then eager calls of every kind that need more room: what the graph works in stays."""
+    J, D, B = 256, 192, 64
+    W0 = dev(S.sc_dictionary(J, D, seed=4))
+    X = dev(S.sc_batch(D, B, seed=4))
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ctx = sfb.Context(0)
+        W = W0.clone()
+        U = torch.empty((B, J), dtype=torch.float32, device="cuda:0")
+        V = torch.empty((B, D), dtype=torch.float32, device="cuda:0")
+
+        def step():
+            ctx.sfb_compute_sf(sfb.SFB_SC, W, X, U=U, V=V, lam=0.1, ista_iters=4, power_iters=3)
+            ctx.sfb_apply(W, U, V, -0.01)
+
+        ref = []
+        for _ in range(3):
+            step()
+            side.synchronize()
+            ref.append(W.clone())
+        W.copy_(W0)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+        grown = ctx._ws.numel()
+        grads = [torch.randn(4096, device="cuda:0") for _ in range(3000)]
+        norm = torch.zeros(1, device="cuda:0")
+        blocks = [torch.randn(2, 16, n, device="cuda:0") for n in (D, J)]
+        rows, out = torch.randn(3000, J, device="cuda:0"), torch.empty(3000, D, device="cuda:0")
+        start, which = torch.tensor([0, 3000], device="cuda:0"), torch.zeros(1, dtype=torch.int32, device="cuda:0")
+        M = torch.randn(D, J, device="cuda:0")
+        for k in range(3):
+            ctx.sfb_clip_grads(sfb.TensorList(grads), 1.0, norm)
+            ctx.sfb_adapter_forward(M, rows, start, which, blocks[0], blocks[1], out)
+            assert ctx._ws.numel() > grown
+            junk = [torch.full((grown // 4,), float("nan"), device="cuda:0") for _ in range(8)]      # where the old one was, had it gone
+            side.synchronize()
+            graph.replay()
+            side.synchronize()
+            assert torch.equal(W, ref[k]), "replay %d differs from the eager step" % k
+            assert all(bool(torch.isnan(j).all()) for j in junk)
+    ctx.close()
