@@ -314,11 +314,26 @@ class Context:
         if rc != SFB_OK:
             raise SfbError(rc, "sfb_create")
         self._ws = None
-        self._captured, self._retired = False, []      # whether a graph works in _ws; the workspaces before it that graphs work in
+        self._captured, self._retired = False, []      # whether a graph works in _ws; memory from before it that graphs work in
         self._tables = {}                              # and tables of lists that they read (by their ids)
         self._index = self.device.index or 0
         self._ad, self._rq, self._needs = sfb_adapters(), sfb_requests(), {}
-        self._shadow = None          # (W tensor, buffer tensor)
+        self._graphs = False                           # whether any call has been captured
+        self._shadow = None                            # (W tensor, buffer tensor) of an attached matrix
+
+    # -- the buffer of an attached matrix, on the context's stream -----------------
+    def _attached_buffer(self, need):
+        if self._shadow is not None and self._shadow[1].numel() >= need:
+            return self._shadow[1]
+        with torch.cuda.stream(self.stream):
+            return torch.empty(need, dtype=torch.uint8, device=self.device)
+
+    def _attached(self, W, buf):
+        """A buffer that another one takes the place of stays as long as a captured graph may write to it."""
+        self._graphs = self._graphs or self._capturing()
+        if self._shadow is not None and self._shadow[1] is not buf and self._graphs:
+            self._retired.append(self._shadow[1])
+        self._shadow = None if W is None else (W, buf)          # (W tensor, buffer tensor)
 
     # -- bf16 working copy of W ----------------------------------------------
     def sfb_shadow_attach(self, W):
@@ -327,15 +342,14 @@ class Context:
         need = lib().sfb_shadow_bytes(J, D)
         if need < 0:
             raise SfbError(int(need), "sfb_shadow_bytes")
-        buf = self._shadow[1] if self._shadow is not None and self._shadow[1].numel() >= need else \
-            torch.empty(need, dtype=torch.uint8, device=self.device)
+        buf = self._attached_buffer(need)
         self._check(lib().sfb_shadow_attach(self._h, _ptr(W, "W", dtype=torch.float32), J, D, buf.data_ptr(),
                                             buf.numel()), "sfb_shadow_attach")
-        self._shadow = (W, buf)
+        self._attached(W, buf)
 
     def sfb_shadow_detach(self):
         self._check(lib().sfb_shadow_detach(self._h), "sfb_shadow_detach")
-        self._shadow = None
+        self._attached(None, None)
 
     # -- W kept as two 16-bit planes --------------------------------------------
     def sfb_split_attach(self, W):
@@ -345,19 +359,19 @@ class Context:
         need = lib().sfb_split_bytes(J, D)
         if need < 0:
             raise SfbError(int(need), "sfb_split_bytes")
-        buf = self._shadow[1] if self._shadow is not None and self._shadow[1].numel() >= need else \
-            torch.empty(need, dtype=torch.uint8, device=self.device)
+        buf = self._attached_buffer(need)
         self._check(lib().sfb_split_attach(self._h, _ptr(W, "W", dtype=torch.float32), J, D, buf.data_ptr(),
                                            buf.numel()), "sfb_split_attach")
-        self._shadow = (W, buf)
+        self._attached(W, buf)
 
     def sfb_split_export(self, W):
         """Enqueues the write-back of the current parameters into W's fp32 array."""
+        self._graphs = self._graphs or self._capturing()
         self._check(lib().sfb_split_export(self._h, _ptr(W, "W", dtype=torch.float32)), "sfb_split_export")
 
     def sfb_split_detach(self):
         self._check(lib().sfb_split_detach(self._h), "sfb_split_detach")
-        self._shadow = None
+        self._attached(None, None)
 
     def close(self):
         if self._h:
@@ -436,7 +450,8 @@ class Context:
         if need > (0 if self._ws is None else self._ws.numel()):
             with torch.cuda.stream(self.stream):
                 self.sfb_set_workspace(torch.empty(need, dtype=torch.uint8, device=self.device))
-        self._captured = self._captured or self._capturing()
+        if not self._captured and self._capturing():
+            self._captured = self._graphs = True
 
     def _ensure_workspace(self, model, J, D, batch, W=None):
         need = self.sfb_workspace_bytes(model, J, D, batch)
@@ -490,6 +505,7 @@ class Context:
         N = U.shape[0]
         if U.dtype != V.dtype:
             raise TypeError("U and V must share a dtype")
+        self._graphs = self._graphs or self._capturing()
         rc = lib().sfb_apply_static(self._h, _ptr(W, "W", dtype=torch.float32), J, D, _ptr(U, "U", shape=(N, J)),
                                     _ptr(V, "V", shape=(N, D)), N, _dtype_code(U), float(eta))
         self._check(rc, "sfb_apply_static")
@@ -688,6 +704,7 @@ class Context:
 
     def sfb_prox_rows(self, W, mode=SFB_PROX_PROJECT):
         J, D = W.shape
+        self._graphs = self._graphs or self._capturing()
         self._check(lib().sfb_prox_rows(self._h, _ptr(W, "W", dtype=torch.float32), J, D, mode), "sfb_prox_rows")
 
 

@@ -180,3 +180,34 @@ def holds(ctx, memory):
             return any(within(x) for x in v)
         return v is memory
     return within(vars(ctx))
+
+
+ATTACHED = {"copy": ("sfb_shadow_attach", "sfb_shadow_detach", "sfb_shadow_bytes"),
+            "planes": ("sfb_split_attach", "sfb_split_detach", "sfb_split_bytes")}
+
+
+@pytest.mark.parametrize("layout", ATTACHED)
+@pytest.mark.parametrize("captured", [None, apply, lambda ctx: ctx.sfb_prox_rows(torch.zeros(8, 8)),
+                                      lambda ctx: ctx.sfb_apply_static(*(torch.zeros(8, 8) for _ in "WUV"), 1.0),
+                                      lambda ctx: ctx.sfb_split_export(torch.zeros(8, 8))])
+@pytest.mark.parametrize("larger", [True, False])
+def test_buffer_of_an_attached_matrix(machine, layout, captured, larger):
+    """It is the context's stream's memory, or known to be used there, and stays while a captured graph may write to it."""
+    attach, detach, query = ATTACHED[layout]
+    ctx = sfb.Context(0, stream=machine.side)
+    W = torch.zeros(8, 8)
+    machine.bytes[query] = 100
+    getattr(ctx, attach)(W)
+    first = ctx._shadow[1]
+    if captured:
+        with machine.capture(machine.side):
+            captured(ctx)
+    if larger:
+        machine.bytes[query] = 1000
+        getattr(ctx, attach)(torch.zeros(8, 80))
+        assert ctx._shadow[1] is not first
+    else:
+        getattr(ctx, detach)()
+        assert ctx._shadow is None
+    assert holds(ctx, first) == (captured is not None)
+    assert captured or first.stream is machine.side or machine.side in first.used_on
