@@ -14,7 +14,8 @@
 // The blocks' part comes first and is what the accumulators start from.  H is held as two bf16 terms side by side along k
 // against the same factors: 16 pairs are one MFMA of k = 32.  Per block that occurs in a tile its factors are loaded and
 // multiplied with the rows that use it; the others' H counts as zeros there.  A factor that is not finite must not meet those
-// zeros: it counts as zero too, and the rows that use it get its products when they are stored.
+// zeros: it counts as zero too, as does an H that is not finite, which must not meet these, and the rows that use the block get
+// the products of either when they are stored.
 //
 // The matrix pipes bound it where there are tiles enough: 8192 rows, 4096 x 4096 with 16 blocks of 16 pairs in 210 to 227 us
 // either way (1.2 to 1.3 PFLOP/s; the library's product alone 207 to 219, along W's rows 251).  What a tile costs besides its k-loop is instructions that are executed once, so their number
@@ -359,7 +360,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
                             least = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, least),
                                                                                            __builtin_bit_cast(u16x2, ~w & 0x7f807f80u)));
                         }
-                    if (__builtin_amdgcn_ballot_w64((least & 0xffffu) == 0 || least >> 16 == 0)) {
+                    const bool not_finite = __builtin_amdgcn_ballot_w64((least & 0xffffu) == 0 || least >> 16 == 0) != 0;
+                    if (not_finite) {
                         special = true;
 #pragma unroll
                         for (int t = 0; t < TN; ++t)
@@ -376,6 +378,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
                         if (__builtin_amdgcn_ballot_w64(mine[ta] == a) == 0) continue;
                         u32x4 ha = {0u, 0u, 0u, 0u};
                         if (mine[ta] == a) ha = h[ta];
+                        if (not_finite) {          // (here, a row at a time: done to h itself it costs the large tiles 31 spilled registers)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                if ((~ha[e] & 0x7f80u) == 0) ha[e] &= 0xffff0000u;
+                                if ((~ha[e] & 0x7f800000u) == 0) ha[e] &= 0xffffu;
+                            }
+                        }
 #pragma unroll
                         for (int tb = 0; tb < TN; ++tb)
                             acc[ta][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f[tb]), __builtin_bit_cast(bf16x8, ha), acc[ta][tb], 0, 0, 0);
@@ -385,8 +394,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
         }
         return special;
     };
-    // The products with factors that are not finite, which none of the stored sums has: an infinity or a not-a-number each, so
-    // the sum's rounding does not matter.  The lanes go through their own pieces of the tile once more.
+    // The products that have a factor or an H that is not finite, an infinity or a not-a-number each, so that the sum's rounding
+    // does not matter: no stored sum has those with such factors; those with such an H some sums have, and once more they change
+    // nothing there.  The lanes go through their own pieces of the tile once more.
     auto add_special = [&](int64_t m0, int64_t n0) {
         const int pitch = adapter_pitch(p.rank), lane = here(threadIdx.x & 63), l16 = lane & 15, quad = lane >> 4;
 #pragma unroll 1
@@ -400,10 +410,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
 #pragma unroll 1
             for (int r = 0; r < rank; ++r) {
                 const float h = p.H[m * pitch + r];
+                const bool all = (~__float_as_uint(h) & 0x7f800000u) == 0;
 #pragma unroll 1
                 for (int e = 0; e < 8; ++e) {
                     const uint32_t bits = (uint32_t)p.F[((int64_t)a * p.rank + r) * p.N + n + e] << 16;
-                    if ((~bits & 0x7f800000u) == 0)
+                    if (all || (~bits & 0x7f800000u) == 0)
                         out[e] = (uint16_t)pack_bf16(fmaf(h, __uint_as_float(bits), __uint_as_float((uint32_t)out[e] << 16)), 0.f);
                 }
             }

@@ -517,3 +517,60 @@ def test_training_steps(sfb, dtype, T):
                 assert torch.equal(p, e), k
             assert torch.isfinite(torch.randn(1 << 16, device="cuda:0").sum()).item()
     own.close()
+
+
+def same_kind(got, want):
+    """Not-a-numbers and infinities of either sign in the same places."""
+    got, want = got.double().cpu().numpy(), np.asarray(want, dtype=np.float64)
+    assert int((np.isnan(got) != np.isnan(want)).sum()) == 0
+    for sign in (1, -1):
+        assert int(((got == sign * np.inf) != (want == sign * np.inf)).sum()) == 0, sign
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,J,D,S", [(24, 136, 200, 5), (300, 136, 200, 9), (700, 136, 200, 9), (700, 40, 136, 700), (4200, 4104, 40, 60),
+                                     (4200, 40, 4104, 60), (8100, 4088, 264, 9), (8100, 264, 4088, 9)])
+def test_infinities_of_factors_and_of_projections(ctx, dtype, T, J, D, S):
+    """A projection that overflows meets a factor that is infinite, zero or finite: what fp32 products and sums make of it, in
+    this row alone, whichever kernel a batch of this size takes."""
+    n, R, r = 3, 20, 17
+    c = A.make(T, J, D, n, R, S, dtype, seed=T + J, single=S == T, none=0)
+    c["ranks"][:] = R
+    c["adapter"] = (torch.arange(S) % n).to(torch.int32)
+    c["scale"][:] = 1.0
+    by, every = A.rows_of(c)
+    huge = [by[1][0], by[1][-1], by[2][len(by[2]) // 2]]
+    for x, v in (("X", "V"), ("dY", "U")):                # row by row: projections of pair r are +-inf, the shared product stays finite
+        c[v][:, :, 7] = 0
+        c[v][:, r, 7] = 1e3
+        c[x][:, 7] = 0
+        c[x][huge, 7] = torch.tensor([2e38, -2e38, 2e38], dtype=dtype)
+    c["W"][:, 7] *= 2.0 ** -20
+    c["W"][7] *= 2.0 ** -20
+    ref = {}
+    for x, v, u, out in (("X", "V", "U", "Y"), ("dY", "U", "V", "dX")):
+        e = dict(c, **{k: c[k].clone() for k in ("U", "V")})
+        e[u][1, r, 3], e[u][1, r, 5], e[u][1, r, 11], e[u][1, r, 13], e[u][1, 2, 20] = float("inf"), float("-inf"), 0, float("nan"), float("inf")
+        e[u][2, r, 3] = float("-inf")
+        d, o = to_dev(e), outputs(e)
+        h = torch.zeros(T, R, dtype=torch.float64)
+        if out == "Y":
+            forward(ctx, d, o)
+            assert torch.equal(torch.isinf(o["H"]).nonzero().cpu(), torch.tensor([[t, r] for t in sorted(huge)]))
+            W = c["W"].double().t()
+        else:
+            ctx.sfb_adapter_backward(d["W"], d["X"], d["dY"], d["start"], d["adapter"], d["U"], d["V"], o["dX"], ranks=d["ranks"], scale=d["scale"])
+            W = c["W"].double()
+        base = c[x].double() @ W
+        for a in range(n):
+            t = by[a]
+            # (in fp32 the projection of a huge row overflows; everything else is far from that)
+            h[t] = c[x][t].double() @ c[v][a].double().t()
+            big = h[t].abs() > 1e39
+            h[t] = torch.where(big, torch.sign(h[t]) * float("inf"), h[t])
+        ref = base.clone()
+        for a in range(n):
+            t = torch.tensor(by[a])
+            for k in range(R):
+                ref[t] += h[t][:, k:k + 1] * e[u][a, k].double()[None, :]
+        same_kind(o[out][every], ref[every].numpy())
