@@ -849,6 +849,24 @@ hipError_t launch_adapter_project_tiles(const ProjectParams& p, DeviceInfo& dev,
     return rt == 1 ? launch_project_tiles<1>(p, dev, stream) : rt == 2 ? launch_project_tiles<2>(p, dev, stream) : launch_project_tiles<4>(p, dev, stream);
 }
 
+// Time of the product of few rows with `factors` more columns and the parts of k that it is best made in, in us: rounds of 512
+// workgroups of so many slices, 0.5 us each, and 3 us around them; planes that are written and read at 4 TB/s.  (64 rows, 4096 x
+// 4096: one part 34 us, four 21.7, six 21.5, sixteen 27; the model takes seven, 21.9.)
+static double few_us(int64_t M, int64_t N, int64_t K, int64_t factors, int tile_m, int* split)
+{
+    const int64_t tiles = ((M + tile_m - 1) / tile_m) * ((N + 63) / 64 + (factors + 63) / 64), slices = (K + BK - 1) / BK;
+    const int64_t width = N + (factors + 3) / 4 * 4;
+    double best = 0;
+    for (int s = 1; s <= 16 && (s == 1 || slices / s >= 4); ++s) {
+        const double us = (double)((tiles * s + 511) / 512) * (0.5 * (double)((slices + s - 1) / s) + 3.0) + (double)(s * M * width) * 8e-6 / 4.0;
+        if (s == 1 || us < best) {
+            best = us;
+            *split = s;
+        }
+    }
+    return best;
+}
+
 AdapterFewPlan adapter_few_plan(int64_t M, int64_t N, int64_t K, int64_t factors)
 {
     AdapterFewPlan f;
@@ -856,22 +874,17 @@ AdapterFewPlan adapter_few_plan(int64_t M, int64_t N, int64_t K, int64_t factors
     // projections of their own 47), 512 rows 54 (54); 8192 x 8192, 128 rows 61 (70), 192 rows 95 (81)
     f.few = M > 0 && (M <= 128 || (M <= 512 && (M + 127) / 128 * 128 * N * K < (int64_t(1) << 33)));
     if (!f.few) return f;
-    // The factors of the whole pool at 4 TB/s, or a launch of its own for those that are used.  64 rows, 4096 x 4096, blocks of 16
-    // pairs: 256 of them 24 us with and 31 without, 384 29 and 31, 512 37 and 31; 1024 x 1024: 512 of them 18 and 20, 1024 21 and 20.
-    f.dense = (double)(factors * K) * 2e-6 / 4.0 <= 5.5 + 1.4e-3 * (double)K;
-    f.width = N + (f.dense ? (factors + 3) / 4 * 4 : 0);
     f.tile_m = M <= 64 ? 64 : 128;      // (65 rows, 4096 x 4096: 22 us, on two tiles of 64 rows 29)
-    // The parts of k: rounds of 512 workgroups of so many slices, 0.5 us each, and 3 us around them; planes that are written and
-    // read at 4 TB/s.  (64 rows, 4096 x 4096: one part 34 us, four 21.7, six 21.5, sixteen 27; the model takes seven, 21.9.)
-    const int64_t tiles = ((M + f.tile_m - 1) / f.tile_m) * ((N + 63) / 64 + (f.dense ? (factors + 63) / 64 : 0)), slices = (K + BK - 1) / BK;
-    double best = 0;
-    for (int s = 1; s <= 16 && (s == 1 || slices / s >= 4); ++s) {
-        const double us = (double)((tiles * s + 511) / 512) * (0.5 * (double)((slices + s - 1) / s) + 3.0) + (double)(s * M * f.width) * 8e-6 / 4.0;
-        if (s == 1 || us < best) {
-            best = us;
-            f.split = s;
-        }
-    }
+    // The factors of the whole pool as further columns, which take what the model says or their own bytes at 4 TB/s, or a launch of
+    // its own for those that are used.  us of a call from a graph, blocks of 16 pairs, further columns / a launch: 64 rows, 4096
+    // x 4096, 256 blocks 24 / 31, 512 of them 37 / 31; 64 rows, 1024 x 1024, 256 blocks 11.7 / 13.5, 800 14.9 / 13.3; 256 rows, 1024
+    // x 1024, 64 blocks 13.4 / 16.5, 256 16.8 / 16.5; 512 rows, 512 x 512, 64 blocks 11.9 / 14.1, 256 16.1 / 14.8, 800 26.9 / 14.2; 512
+    // rows, 2048 x 2048, 64 blocks 23.3 / 26.8, 256 35.3 / 27.3, 800 61 / 27 (no wrong choice on 56 sizes from 1 to 512 rows).
+    int with = 1, without = 1;
+    const double more = few_us(M, N, K, factors, f.tile_m, &with) - few_us(M, N, K, 0, f.tile_m, &without);
+    f.dense = std::max(more, (double)(factors * K) * 2e-6 / 4.0) <= 3.0 + 1.7e-3 * (double)K;
+    f.split = f.dense ? with : without;
+    f.width = N + (f.dense ? (factors + 3) / 4 * 4 : 0);
     return f;
 }
 

@@ -73,3 +73,14 @@ def split(lib, kind, B, J, D):
 
 def estimate(lib, kind, B, J, D):
     return _plan(lib, kind, B, J, D).us
+
+
+class _FewPlan(ctypes.Structure):        # AdapterFewPlan of csrc/adapter.h
+    _fields_ = [("few", ctypes.c_bool), ("dense", ctypes.c_bool), ("split", ctypes.c_int), ("tile_m", ctypes.c_int), ("width", ctypes.c_int64)]
+
+
+def adapter_few(lib, M, N, K, factors):
+    """The plan of an adapter call's product of M bf16 rows, N columns and K terms beside a pool of so many factors."""
+    f = lib._ZN3sfb16adapter_few_planEllll
+    f.restype, f.argtypes = _FewPlan, [ctypes.c_int64] * 4
+    return f(M, N, K, factors)

@@ -574,3 +574,19 @@ def test_infinities_of_factors_and_of_projections(ctx, dtype, T, J, D, S):
             for k in range(R):
                 ref[t] += h[t][:, k:k + 1] * e[u][a, k].double()[None, :]
         same_kind(o[out][every], ref[every].numpy())
+
+
+# T, J, D, n, R, S, whether the pool's factors are further columns of the product
+POOLS = [(512, 512, 512, 64, 16, 8, True), (512, 512, 512, 64, 128, 8, False), (256, 520, 1032, 64, 16, 30, True), (256, 520, 1032, 500, 16, 30, False),
+         (512, 64, 64, 1500, 16, 512, False), (40, 264, 1000, 900, 16, 40, False), (1, 136, 1024, 1500, 16, 1, False)]
+
+
+@pytest.mark.parametrize("case", POOLS)
+def test_pools_on_both_sides(ctx, case):
+    """Few rows beside pools small enough to be multiplied whole, and larger ones."""
+    T, J, D, n, R, S, _ = case
+    c = A.poison(A.make(T, J, D, n, R, S, BF16, seed=T + n, single=S == T))
+    d, o = to_dev(c), outputs(c)
+    forward(ctx, d, o)
+    backward(ctx, d, o)
+    compare(c, o)

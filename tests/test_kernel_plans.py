@@ -1,4 +1,5 @@
 """The shapes of the GPU tests reach the kernel instantiations that those tests are there for (the planners run on the host)."""
+import ctypes
 import os
 
 import pytest
@@ -77,3 +78,25 @@ def test_adding_up_elsewhere_is_cheaper(lib):
         first = {kind: next(D for D in range(256, 40000, 32) if K.split(lib, kind, B, J, D) > 1) for kind in ("projections", "shrink")}
         assert first["projections"] < first["shrink"], (B, J, first)
         assert all(K.estimate(lib, "projections", B, J, D) <= K.estimate(lib, "shrink", B, J, D) for D in range(32, 10000, 500))
+
+
+def test_adapter_pools_of_few_rows(lib):
+    """Further columns of the product only where they cost less than a launch for the factors in use: rows, their tiles and the
+    planes count, not the bytes of the factors alone.  (Both sides measured at these sizes.)"""
+    from test_gpu_adapter import POOLS
+    assert [K.adapter_few(lib, T, J, D, n * R).dense for T, J, D, n, R, _, _ in POOLS] == [dense for *_, dense in POOLS]
+    assert all(K.adapter_few(lib, T, J, D, n * R).few for T, J, D, n, R, _, _ in POOLS)
+    for M, N, D, factors in ((1, 1024, 1024, 64), (64, 4096, 4096, 512), (64, 4096, 4096, 4096), (128, 4096, 4096, 4096), (200, 1000, 520, 24),
+                             (512, 2048, 2048, 1024)):
+        assert K.adapter_few(lib, M, N, D, factors).dense
+    for M, N, D, factors in ((64, 4096, 4096, 8192), (512, 2048, 2048, 4096), (256, 1024, 1024, 12800), (1, 1024, 1024, 24000)):
+        assert not K.adapter_few(lib, M, N, D, factors).dense
+
+
+def test_workspace_of_a_large_adapter_pool(lib):
+    """512 rows of 8 columns beside 65536 blocks of 16 pairs: the rows' projections, not a plane of the whole pool."""
+    import paper_1409_5705_amd as sfb
+    ad = sfb.binding.sfb_adapters()
+    ad.count, ad.rank, ad.dtype = 65536, 16, sfb.SFB_BF16
+    for query in (lib.sfb_adapter_forward_workspace_bytes, lib.sfb_adapter_backward_workspace_bytes):
+        assert 0 < query(8, 8, 512, ctypes.byref(ad)) < 1 << 20
