@@ -377,7 +377,7 @@ typedef struct {
  * wanted), overwritten whole: blocks without rows and pairs that are not in use get zeros.  H: what the forward pass gave, or
  * NULL (computed again).  The gradient of W itself is the factor pair (dY, X): sfb_apply takes it as it is.
  * Rows of no request contribute nothing, whatever they hold.  Every sum is made in a fixed order: equal calls give equal bits.
- * Outputs must not overlap inputs.  The workspace queries give the bytes that a call of these
+ * An output that shares a byte with an input or another output is refused.  The workspace queries give the bytes that a call of these
  * sizes needs; the workspace holds nothing between calls.
  */
 int64_t sfb_adapter_forward_workspace_bytes(int64_t J, int64_t D, int64_t T, const sfb_adapters* adapters);

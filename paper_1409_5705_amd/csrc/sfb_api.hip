@@ -5,6 +5,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <initializer_list>
 #include <new>
 
 #include "adapter.h"
@@ -1101,6 +1102,37 @@ static int check_adapter_call(const sfb_ctx* ctx, const void* W, int32_t w_dtype
     return SFB_OK;
 }
 
+// A call's array; null: it has none.
+struct Span {
+    const void* at;
+    uint64_t bytes;
+};
+static bool share_bytes(const Span& a, const Span& b)
+{
+    if (!a.at || !b.at || a.bytes == 0 || b.bytes == 0) return false;
+    const uint64_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+    return x >= y ? x - y < b.bytes : y - x < a.bytes;
+}
+// Whether no output of a call shares a byte with one of its inputs or with another output: kernels read some while they write
+// others.  rows: what the call reads per row beside X (dY, H).
+static bool outputs_apart(std::initializer_list<Span> out, std::initializer_list<Span> rows, const void* W, int32_t w_dtype, int64_t J,
+                          int64_t D, const sfb_adapters* ad, const sfb_requests* rq)
+{
+    const uint64_t e = ad->dtype == SFB_BF16 ? 2 : 4, pairs = (uint64_t)ad->count * (uint64_t)ad->rank;
+    const Span shared[] = {{W, (uint64_t)J * (uint64_t)D * (w_dtype == SFB_BF16 ? 2 : 4)}, {ad->U, pairs * (uint64_t)J * e}, {ad->V, pairs * (uint64_t)D * e},
+                           {ad->ranks, (uint64_t)ad->count * 4}, {ad->scale, (uint64_t)ad->count * 4},
+                           {rq->start, ((uint64_t)rq->count + 1) * 8}, {rq->adapter, (uint64_t)rq->count * 4}};
+    for (const Span& o : out) {
+        for (const Span& in : shared)
+            if (share_bytes(o, in)) return false;
+        for (const Span& in : rows)
+            if (share_bytes(o, in)) return false;
+        for (const Span& other : out)
+            if (&other != &o && share_bytes(o, other)) return false;
+    }
+    return true;
+}
+
 static sfb::AdapterProjectArgs project_args(sfb_ctx* ctx, int64_t T, const sfb_adapters* ad, const sfb_requests* rq)
 {
     sfb::AdapterProjectArgs a = {};
@@ -1228,6 +1260,9 @@ int sfb_adapter_forward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J,
     if (!X || !Y || !aligned16(X) || !aligned16(Y)) return SFB_EINVAL;
     const AdapterLayout l = adapter_layout(T, J, D, ad, false);
     if (!ctx->ws || ctx->ws_bytes < l.total) return SFB_ENOWS;
+    const uint64_t e = ad->dtype == SFB_BF16 ? 2 : 4;
+    if (!outputs_apart({{Y, (uint64_t)(T * J) * e}, {H, (uint64_t)(T * ad->rank) * 4}}, {{X, (uint64_t)(T * D) * e}}, W, w_dtype, J, D, ad, rq))
+        return SFB_EINVAL;
     const DeviceScope scope(ctx->device);
     SFB_TRY(scope.status);
     return adapter_output(ctx, l, X, W, Wb, blocked, false, T, J, D, ad, rq, ad->V, ad->U, reinterpret_cast<float*>(ctx->ws + l.off_h), H, Y);
@@ -1248,6 +1283,10 @@ int sfb_adapter_backward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J
     if (!rows) T = 0;
     const AdapterLayout l = adapter_layout(T, D, J, ad, true);
     if (rows && (!ctx->ws || ctx->ws_bytes < l.total)) return SFB_ENOWS;
+    const uint64_t e = ad->dtype == SFB_BF16 ? 2 : 4, pairs = (uint64_t)ad->count * (uint64_t)ad->rank * 4;
+    if (!outputs_apart({{dX, (uint64_t)(T * D) * e}, {dU, pairs * (uint64_t)J}, {dV, pairs * (uint64_t)D}},
+                       {{X, (uint64_t)(T * D) * e}, {dY, (uint64_t)(T * J) * e}, {H, (uint64_t)(T * ad->rank) * 4}}, W, w_dtype, J, D, ad, rq))
+        return SFB_EINVAL;
     const DeviceScope scope(ctx->device);
     SFB_TRY(scope.status);
     sfb::AdapterProjectArgs a = project_args(ctx, T, ad, rq);

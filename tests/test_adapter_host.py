@@ -137,3 +137,42 @@ def test_table_of_a_list(sfb):
     assert [words[i] for i in range(8)] == [0, 1, 2, 4, 7, 8, 8, 8]
     bf16 = 1 << 31
     assert [words[8 + i] for i in range(5)] == [5, 4096, 1 | bf16, 808 | bf16, 1]
+
+
+# places that are far apart, and what lies there in a call of T = 10 rows, J = 64, D = 72, three blocks of 8 pairs, two requests
+FAR = {k: (i + 1) << 32 for i, k in enumerate(("W", "X", "dY", "U", "V", "ranks", "scale", "start", "adapter", "Y", "H", "dX", "dU", "dV", "ws"))}
+SIZE = dict(W=64 * 72 * 2, X=10 * 72 * 2, dY=10 * 64 * 2, U=3 * 8 * 64 * 2, V=3 * 8 * 72 * 2, ranks=12, scale=12, start=24, adapter=8, Y=10 * 64 * 2,
+            H=10 * 8 * 4, dX=10 * 72 * 2, dU=3 * 8 * 64 * 4, dV=3 * 8 * 72 * 4)
+
+
+def placed(sfb, call, where):
+    """The call with its arrays at these addresses (SFB_EHIP: it was accepted, and there is no device here)."""
+    own = ctypes.create_string_buffer(8192)
+    assert sfb.lib().sfb_set_workspace(own, where["ws"], 1 << 40) == sfb.SFB_OK
+    ad = adapters(sfb, **{k: where[k] for k in ("U", "V", "ranks", "scale")})
+    rq = requests(sfb, start=where["start"], adapter=where["adapter"])
+    names = ("W", "X", "Y", "H") if call is forward else ("W", "X", "dY", "H", "dX", "dU", "dV")
+    return call(sfb, own, ad=ad, rq=rq, **{k: where[k] for k in names})
+
+
+@pytest.mark.parametrize("call,outputs", [(forward, ("Y", "H")), (backward, ("dX", "dU", "dV"))])
+def test_outputs_over_inputs(sfb, call, outputs):
+    """An output that shares a byte with an input or with another output is refused; one right behind or in front of it is not."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("for machines without a device: what is accepted is launched")
+    assert placed(sfb, call, FAR) == sfb.SFB_EHIP
+    inputs = {"W", "X", "U", "V", "ranks", "scale", "start", "adapter"} | ({"dY", "H"} if call is backward else set())
+    for out in outputs:
+        for other in (inputs | set(outputs)) - {out}:
+            at, size, mine = FAR[other], SIZE[other], SIZE[out]
+            for place in (at, at + (size - 1) // 16 * 16, at - (mine - 1) // 16 * 16):
+                assert placed(sfb, call, dict(FAR, **{out: place})) == sfb.SFB_EINVAL, (out, other, place - at)
+            for place in (at + (size + 15) // 16 * 16, at - (mine + 15) // 16 * 16):
+                assert placed(sfb, call, dict(FAR, **{out: place})) == sfb.SFB_EHIP, (out, other, place - at)
+    # what a call does not write, or does not have, cannot be in the way
+    if call is forward:
+        assert placed(sfb, call, dict(FAR, H=None)) == sfb.SFB_EHIP
+    else:
+        assert placed(sfb, call, dict(FAR, dX=None)) == sfb.SFB_EHIP and placed(sfb, call, dict(FAR, dU=None, dV=None)) == sfb.SFB_EHIP
+        assert placed(sfb, call, dict(FAR, dX=FAR["X"], dU=None, dV=None)) == sfb.SFB_EINVAL

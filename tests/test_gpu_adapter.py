@@ -590,3 +590,25 @@ def test_pools_on_both_sides(ctx, case):
     forward(ctx, d, o)
     backward(ctx, d, o)
     compare(c, o)
+
+
+def test_output_that_overlaps(sfb, ctx):
+    """Views that share some rows with an input, and an output of another type at an input's place."""
+    T, D, R = 20, 64, 64
+    for dtype in (BF16, F32):
+        c = A.make(T, 64, D, 2, R, 3, dtype, seed=1)
+        d, o = to_dev(c), outputs(c)
+        wide = torch.full((T + 8, D), SENTINEL, dtype=dtype, device="cuda:0")
+        wide[:T] = d["X"]
+        d["X"] = wide[:T]
+        calls = [lambda: forward(ctx, d, dict(o, Y=wide[8:])), lambda: forward(ctx, d, dict(o, Y=d["W"][:T])),
+                 lambda: backward(ctx, d, dict(o, dX=wide[8:])), lambda: backward(ctx, d, dict(o, dV=o["dU"]))]
+        if dtype == F32:
+            calls += [lambda: forward(ctx, d, dict(o, H=d["X"])), lambda: backward(ctx, d, o, H=o["dX"]), lambda: forward(ctx, d, dict(o, H=o["Y"]))]
+        for call in calls:
+            with pytest.raises((ValueError, sfb.SfbError)) as err:
+                call()
+            assert err.type is ValueError or err.value.code == sfb.SFB_EINVAL
+        torch.cuda.synchronize()
+        assert torch.equal(wide[:T].cpu(), c["X"]) and bool((wide[T:] == wide.new_full((1,), SENTINEL)).all())
+        assert bool((o["dU"] == SENTINEL).all()) and torch.equal(d["W"].cpu(), c["W"])
