@@ -1367,6 +1367,11 @@ static int grad_norm_impl(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, c
     const int rc = check_list(list, count, clip);
     if (rc != SFB_OK) return rc;
     if (!ctx->ws || ctx->ws_bytes < round_up((sfb::grad_norm_partials(list, count) + 1) * 8)) return SFB_ENOWS;
+    for (int64_t i = 0; clip && i < count; ++i) {
+        const uint64_t bytes = (uint64_t)list[i].n * (list[i].dtype == SFB_BF16 ? 2 : 4);
+        const Span src = {list[i].src, bytes}, dst = {list[i].dst, bytes}, of_norm = {norm, 4};
+        if (share_bytes(src, of_norm) || share_bytes(dst, of_norm) || (src.at != dst.at && share_bytes(src, dst))) return SFB_EINVAL;
+    }
     const DeviceScope scope(ctx->device);
     SFB_TRY(scope.status);
     double* partial = reinterpret_cast<double*>(ctx->ws);

@@ -176,3 +176,31 @@ def test_outputs_over_inputs(sfb, call, outputs):
     else:
         assert placed(sfb, call, dict(FAR, dX=None)) == sfb.SFB_EHIP and placed(sfb, call, dict(FAR, dU=None, dV=None)) == sfb.SFB_EHIP
         assert placed(sfb, call, dict(FAR, dX=FAR["X"], dU=None, dV=None)) == sfb.SFB_EINVAL
+
+
+def test_clipping_over_its_own_inputs(sfb):
+    """The norm inside a tensor that is scaled, or a tensor that is scaled into a part of itself."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("for machines without a device: what is accepted is launched")
+    L, far = sfb.lib(), 1 << 32
+    own = ctypes.create_string_buffer(8192)
+    assert L.sfb_set_workspace(own, 1 << 40, 1 << 20) == sfb.SFB_OK
+
+    def clip(norm, *rows):
+        t = (sfb.binding.sfb_tensor * len(rows))()
+        for k, (src, dst, n, dtype) in enumerate(rows):
+            t[k].src, t[k].dst, t[k].n, t[k].dtype = src, dst, n, dtype
+        return L.sfb_clip_grads(own, t, len(rows), None, 1.0, norm), L.sfb_grad_norm(own, t, len(rows), None, norm)
+
+    accepted, refused = sfb.SFB_EHIP, sfb.SFB_EINVAL          # (accepted: there is no device here)
+    a, b = (far, far, 100, 0), (2 * far, 3 * far, 50, 1)
+    for norm in (4 * far, far + 400, far - 4, 2 * far + 100, 3 * far - 4, 3 * far + 100):
+        assert clip(norm, a, b) == (accepted, accepted), norm
+    for norm in (far, far + 396, 2 * far, 2 * far + 96, 3 * far, 3 * far + 96):
+        assert clip(norm, a, b) == (refused, accepted), norm          # (the norm alone is written after everything is read)
+    for dst in (far + 4, far + 396, far - 396):
+        assert clip(4 * far, (far, dst, 100, 0)) == (refused, accepted), dst
+    for dst in (far, far + 400, far - 400):
+        assert clip(4 * far, (far, dst, 100, 0)) == (accepted, accepted), dst
+    assert clip(far, (far, far, 0, 0), b) == (accepted, accepted)          # a tensor of no elements is nowhere
