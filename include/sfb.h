@@ -394,8 +394,10 @@ int sfb_adapter_backward(sfb_ctx* ctx, const void* W, int32_t w_dtype, int64_t J
  *       norm = sqrt(sum_i sum_k g_i[k]^2),      dst_i[k] = src_i[k] * min(1, max_norm / norm).
  * sfb_grad_norm writes *norm (device); it does not look at dst.  sfb_clip_grads does both; dst_i may be src_i (scaled in
  * place, and left alone where the norm is within the bound) or another tensor (always written), otherwise tensors must not
- * overlap, and *norm must not lie in one (dst_i that shares a part with src_i, and such a norm, are refused).  Squares are summed in 64 bits in a fixed order.  max_norm >= 0.  A norm that is not finite is reported as it is,
- * and the scale is then 0 (infinite) or not a number: look at *norm before the gradients are used.
+ * overlap, and *norm must not lie in one (dst_i that shares a part with src_i, and such a norm, are refused).  Squares are summed
+ * in 64 bits in a fixed order, and the scale is held in 64 bits.  max_norm >= 0.  A sum that is not finite is reported as it is, and
+ * the scale is then 0 (infinite) or not a number: look at *norm before the gradients are used.  A finite norm beyond the range of
+ * fp32 is reported as infinite, too, and clipped as what it is.
  * Needs the workspace of sfb_grad_norm_workspace_bytes.
  * table (may be NULL): the list's description in device memory, for lists of more tensors than a launch takes as its arguments
  * (240, clipping 160): with it a pass is one launch whatever their number.  The caller has sfb_tensor_table_fill write it

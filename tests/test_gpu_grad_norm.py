@@ -281,3 +281,25 @@ def test_captured_list_is_gone(sfb):
         assert abs(norm.item() - want) <= 2.0 ** -24 * want * 1.001
         check_clipped([src], [flat], 1.0 / want)
     own.close()
+
+
+@pytest.mark.parametrize("bound", [1.0, 0.3125, 2.0 ** -100, 2.0 ** -140])
+@pytest.mark.parametrize("size", [1.0, 2.0 ** 70, 2.0 ** -70])
+def test_clipped_to_half_a_step(sfb, ctx, bound, size):
+    """The scale is held in 64 bits and a result rounded once (bf16: to fp32 before): the error is half a step of its type, with a
+    scale of 32 bits it would be twice that of an fp32 result."""
+    src = [t.mul_(size) for t in tensors([100_000, 70_001, 33], seed=3)]
+    want = norm64(src)
+    norm = torch.zeros(1, device="cuda:0")
+    dst = [torch.zeros_like(t) for t in src]
+    ctx.sfb_clip_grads(sfb.TensorList(src, dst), bound, norm)          # (bound is an fp32 number)
+    assert abs(norm.item() - want) <= (2.0 ** -24 + 2.0 ** -36) * want + 2.0 ** -150
+    coef = bound / want
+    assert coef < 1.0 or size < 1.0
+    for s, d in zip(src, dst):
+        exact = s.double() * min(1.0, coef)
+        # 2^-36: the sum of 1.7e5 squares is off by 1.7e5 2^-53 at most, its root by half of that; the last term: half a denormal step
+        room = exact.abs() * (2.0 ** -24 + 2.0 ** -36) + 2.0 ** -150
+        if s.dtype == BF16:
+            room += exact.abs() * 2.0 ** -8 * 1.001 + 2.0 ** -134
+        assert bool(((d.double() - exact).abs() <= room).all())
