@@ -306,17 +306,17 @@ class Context:
 
     def __init__(self, device=0, stream=None):
         self._h = ctypes.c_void_p()
-        self.device = torch.device("cuda", device) if isinstance(device, int) else torch.device(device)
+        self.device = torch.device("cuda", device if isinstance(device, int) else torch.device(device).index or 0)
         if stream is None:
             stream = torch.cuda.current_stream(self.device)
         self.stream = stream
-        rc = lib().sfb_create(ctypes.byref(self._h), self.device.index or 0, ctypes.c_void_p(stream.cuda_stream))
+        rc = lib().sfb_create(ctypes.byref(self._h), self.device.index, ctypes.c_void_p(stream.cuda_stream))
         if rc != SFB_OK:
             raise SfbError(rc, "sfb_create")
         self._ws = None
         self._captured, self._retired = False, []      # whether a graph works in _ws; memory from before it that graphs work in
         self._tables = {}                              # and tables of lists that they read (by their ids)
-        self._index = self.device.index or 0
+        self._index = self.device.index
         self._ad, self._rq, self._needs = sfb_adapters(), sfb_requests(), {}
         self._graphs = False                           # whether any call has been captured
         self._shadow = None                            # (W tensor, buffer tensor) of an attached matrix

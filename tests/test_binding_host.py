@@ -211,3 +211,16 @@ def test_buffer_of_an_attached_matrix(machine, layout, captured, larger):
         assert ctx._shadow is None
     assert holds(ctx, first) == (captured is not None)
     assert captured or first.stream is machine.side or machine.side in first.used_on
+
+
+@pytest.mark.parametrize("device", [0, "cuda", "cuda:0", torch.device("cuda")])
+def test_device_without_a_number(machine, device):
+    """"cuda" is the first device, and tensors say so of themselves: a list on it is on the context's device."""
+    ctx = sfb.Context(device, stream=machine.side)
+    assert ctx.device == torch.device("cuda", 0)
+    lst = List(Memory(64, machine.side))
+    lst.device = torch.device("cuda", 0)
+    ctx.sfb_grad_norm(lst, torch.zeros(1))
+    lst.device = torch.device("cuda", 1)
+    with pytest.raises(ValueError):
+        ctx.sfb_grad_norm(lst, torch.zeros(1))
