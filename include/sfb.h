@@ -416,6 +416,9 @@ int sfb_tensor_table_fill(const sfb_tensor* list, int64_t count, void* host);
 int sfb_grad_norm(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, const void* table, float* norm);
 int sfb_clip_grads(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, const void* table, float max_norm, float* norm);
 
+/* 1 while the context's stream is being captured into a HIP graph (the caller then has to keep what the calls work in, the
+ * workspace among it, for as long as the graph is replayed), otherwise 0. */
+int sfb_capturing(sfb_ctx* ctx);
 /* Static description of a status code. */
 const char* sfb_strerror(int code);
 /* hipError_t (as int) of the last failed HIP call on this context, 0 if none. */

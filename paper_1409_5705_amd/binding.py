@@ -162,6 +162,8 @@ def lib():
         L.sfb_grad_norm.restype = ctypes.c_int
         L.sfb_clip_grads.argtypes = [vp, pt, i64, vp, ctypes.c_float, vp]
         L.sfb_clip_grads.restype = ctypes.c_int
+        L.sfb_capturing.argtypes = [vp]
+        L.sfb_capturing.restype = ctypes.c_int
         L.sfb_prox_rows.argtypes = [vp, vp, i64, i64, i32]
         L.sfb_prox_rows.restype = ctypes.c_int
         L.sfb_strerror.argtypes = [ctypes.c_int]
@@ -316,7 +318,8 @@ class Context:
         self._ws = None
         self._captured, self._retired = False, []      # whether a graph works in _ws; memory from before it that graphs work in
         self._tables = {}                              # and tables of lists that they read (by their ids)
-        self._index = self.device.index
+        self._index, self._raw = self.device.index, stream.cuda_stream
+        self._one_device = torch.cuda.device_count() == 1
         self._ad, self._rq, self._needs = sfb_adapters(), sfb_requests(), {}
         self._graphs = False                           # whether any call has been captured
         self._shadow = None                            # (W tensor, buffer tensor) of an attached matrix
@@ -439,10 +442,10 @@ class Context:
 
     def _capturing(self):
         """Whether the context's stream is being captured into a graph."""
-        if torch._C._cuda_getCurrentStream(self._index)[0] == self.stream.stream_id and torch._C._cuda_getDevice() == self._index:
+        # (0.3 us of a small call's 7)
+        if self._one_device and torch._C._cuda_getCurrentRawStream(self._index) == self._raw:
             return torch._C._cuda_isCurrentStreamCapturing()
-        with torch.cuda.stream(self.stream):
-            return torch._C._cuda_isCurrentStreamCapturing()
+        return lib().sfb_capturing(self._h) > 0
 
     def _grow_workspace(self, need):
         """Room for `need` bytes, allocated on the context's stream; every call that takes a workspace comes here.  What a captured

@@ -1391,6 +1391,16 @@ int sfb_clip_grads(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, const vo
     return grad_norm_impl(ctx, list, count, table, true, max_norm, norm);
 }
 
+int sfb_capturing(sfb_ctx* ctx)
+{
+    if (!ctx) return SFB_EINVAL;
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    const hipError_t e = hipStreamIsCapturing(ctx->stream, &status);
+    if (e == hipSuccess) return status != hipStreamCaptureStatusNone;
+    (void)hipGetLastError();
+    return e == hipErrorStreamCaptureImplicit ? 0 : hip_fail(ctx, e);      // (the default stream, which is never captured, beside one that is)
+}
+
 const char* sfb_strerror(int code)
 {
     switch (code) {

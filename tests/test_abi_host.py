@@ -113,3 +113,7 @@ def test_product_never_imports_oracle():
         if f.endswith((".py", ".c")):
             txt = open(os.path.join(ROOT, "oracle", f)).read()
             assert "paper_1409_5705_amd" not in txt and "libsfb.so" not in txt
+
+
+def test_capturing_without_a_context(sfb):
+    assert sfb.lib().sfb_capturing(None) == sfb.SFB_EINVAL

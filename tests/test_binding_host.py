@@ -36,8 +36,15 @@ class Memory:
 class Machine:
     def __init__(self):
         self.default, self.side = Stream(1), Stream(2)
-        self.current, self.captured = self.default, None
+        self.current, self.captured, self.devices = self.default, None, 1
         self.bytes = {"sfb_apply_workspace_bytes": 100, "sfb_workspace_bytes": 100, "sfb_adapter_forward_workspace_bytes": 100}
+
+    def sfb_create(self, handle, device, stream):
+        self.bound = stream.value
+        return 0
+
+    def sfb_capturing(self, handle):
+        return 1 if self.captured is not None and self.captured.cuda_stream == self.bound else 0
 
     def __getattr__(self, name):          # the library: every call succeeds, every query is answered from `bytes`
         if not name.startswith("sfb_"):
@@ -66,8 +73,8 @@ def machine(monkeypatch):
     monkeypatch.setattr(binding.Context, "_at", lambda self, t, *args: id(t))
     monkeypatch.setattr(torch, "empty", lambda size, **kw: Memory(size, m.current))
     monkeypatch.setattr(torch.cuda, "stream", m.on)
-    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
-    monkeypatch.setattr(torch._C, "_cuda_getCurrentStream", lambda index: (m.current.stream_id, index, 1), raising=False)
+    monkeypatch.setattr(torch.cuda, "device_count", lambda: m.devices)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: m.current.cuda_stream, raising=False)
     monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: m.current is m.captured, raising=False)
     return m
 
@@ -99,9 +106,11 @@ def test_table_of_another_stream(machine):
 
 
 @pytest.mark.parametrize("inside", [True, False])
-def test_table_of_a_captured_call(machine, inside):
+@pytest.mark.parametrize("devices", [1, 8])
+def test_table_of_a_captured_call(machine, inside, devices):
     """A graph reads it again at every replay: it stays for as long as the context does, whether the context's stream or another one
     is the current one during the capture."""
+    machine.devices = devices
     ctx = sfb.Context(0, stream=machine.side)
     table = Memory(4096, machine.side)
     other = Memory(4096, machine.side)

@@ -218,3 +218,32 @@ def test_workspace_grows_after_a_captured_step(sfb):
             assert torch.equal(W, ref[k]), "replay %d differs from the eager step" % k
             assert all(bool(torch.isnan(j).all()) for j in junk)
     ctx.close()
+
+
+def test_capturing(sfb):
+    """Of the context's own stream, whichever is the current one."""
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    contexts = [sfb.Context(0, stream=s) for s in (side, other)] + [sfb.Context(0)]
+    x = torch.zeros(8, device="cuda:0")
+    torch.cuda.synchronize()
+
+    def state():
+        lib = [sfb.lib().sfb_capturing(c._h) for c in contexts]
+        assert [int(c._capturing()) for c in contexts] == lib
+        return lib
+
+    assert state() == [0, 0, 0]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side, capture_error_mode="relaxed"):
+        x.add_(1)
+        assert state() == [1, 0, 0]
+        with torch.cuda.stream(other):
+            assert state() == [1, 0, 0]
+    assert state() == [0, 0, 0]
+    x.zero_()
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert x.tolist() == [1.0] * 8
+    for c in contexts:
+        c.close()
