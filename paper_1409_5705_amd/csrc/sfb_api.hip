@@ -1043,10 +1043,10 @@ static AdapterLayout adapter_layout(int64_t T, int64_t N, int64_t K, const sfb_a
 {
     AdapterLayout l;
     // An fp32 contraction of unaligned rows takes 1.7 times as long (777 x 1003 x 2047: 53 us, with K = 2048 31 us): 0.4 of its time
-    // at 60 TFLOP/s against the copies at 3 TB/s and a launch of 4 us.
+    // at 60 TFLOP/s against the copies at 3 TB/s and a launch of 4 us.  (And a launch has less than 2^32 threads, of four elements each.)
     l.Kp = (K + 3) / 4 * 4;
     l.Np = backward ? (N + 3) / 4 * 4 : N;
-    if (ad->dtype == SFB_BF16 || (l.Kp == K && l.Np == N) ||
+    if (ad->dtype == SFB_BF16 || (l.Kp == K && l.Np == N) || (double)(T + l.Np) * (double)l.Kp > 8e9 ||
         0.4 * 2e-6 * (double)T * (double)N * (double)K / 60.0 < 8e-6 * (double)(T + N) * (double)K / 3.0 + 4.0)
         l.Kp = K, l.Np = N;
     const int64_t h = round_up(T * sfb::adapter_pitch(ad->rank) * 4);

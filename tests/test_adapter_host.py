@@ -204,3 +204,15 @@ def test_clipping_over_its_own_inputs(sfb):
     for dst in (far, far + 400, far - 400):
         assert clip(4 * far, (far, dst, 100, 0)) == (accepted, accepted), dst
     assert clip(far, (far, far, 0, 0), b) == (accepted, accepted)          # a tensor of no elements is nowhere
+
+
+@pytest.mark.parametrize("query", ["sfb_adapter_forward_workspace_bytes", "sfb_adapter_backward_workspace_bytes"])
+def test_aligned_copies_that_a_launch_can_make(sfb, query):
+    """fp32 matrices whose rows are not 16-byte aligned are copied to rows that are, up to the 2^32 threads of a launch: larger
+    ones are taken as they lie."""
+    q = getattr(sfb.lib(), query)
+    ad = adapters(sfb, dtype=0)
+    plain = q(1 << 16, 8192, 512, ctypes.byref(ad))
+    assert q(1 << 16, 8191, 512, ctypes.byref(ad)) > plain + (1 << 16) * 8191 * 4
+    plain = q(1 << 21, 8192, 512, ctypes.byref(ad))
+    assert q(1 << 21, 8191, 512, ctypes.byref(ad)) <= plain + (1 << 20)
