@@ -292,8 +292,9 @@ hipError_t launch_adapter_join(const AdapterJoinArgs& a, hipStream_t stream)
     const bool two = a.T * ((a.N + 511) / 512) >= 2048;
     if (!a.bf16) return two ? join_rows<float, 2, 0>(a, stream) : join_rows<float, 1, 0>(a, stream);
     if (two) return join_rows<uint16_t, 2, 0>(a, stream);
-    // (a call of 64 requests, 4096 x 4096, blocks of 16 pairs: 18.4 us, with 16 factors ahead 17.4, with eight 18.6; of 200 rows, 1000 x 520,
-    // blocks of eight pairs: 22.3, with 16 ahead 22.5)
+    // 16 factors ahead, for rows with 9 to 15 pairs in use: the loop takes eight at a time and what is left one after another.  us of a
+    // call with / without: 64 rows, 4096 x 4096, 12 pairs 20.1 / 21.2, 8 to 16 of them 17.5 / 18.5, 16 20.2 / 20.3, 32 22.0 / 22.0, 64 25.7
+    // / 25.5; 64 rows, 2048 x 4096, 12 pairs 17.1 / 18.3; one row, 1024 x 1024, 8 pairs 8.0 / 7.5, 16 8.0 / 7.7, 256 15.4 / 15.0.
     return a.rank > 8 ? join_rows<uint16_t, 1, 16>(a, stream) : join_rows<uint16_t, 1, 0>(a, stream);
 }
 

@@ -457,8 +457,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM == 8 ? 1
 
     // ---- pipeline: slice s lives in stage s & 1; f0 holds the fragments of its first k-step, f1 of the second
     Frags f0, f1;
-    // Small tiles: the first one's blocks come in front of its slices and have all of the LDS for their factors (704 rows, 8192 x
-    // 2048, 40 requests with blocks of 32 pairs: 46 us, with four chunks a round 49).  (On the large ones the order costs registers.)
+    // Small tiles: the first one's blocks come in front of its slices and have all of the LDS for their factors: where a tile has
+    // many of them it gains (704 rows, 8192 x 2048, 40 requests with blocks of 32 pairs: 46 us, with four chunks a round 49; 700
+    // rows, 8192 x 1024, 200 requests, 64 pairs 97 and 113, four pairs 43 and 46), elsewhere nothing (1500 rows, 2048 x 2048, 30
+    // requests, 16 pairs 31 and 31; 2000 rows, 8192 x 512, 8 requests, 128 pairs 54 and 54).  (On the large ones the order costs registers.)
     constexpr bool FIRST = TM == 4 && !SPLIT;
     auto prologue = [&]() {
         enter_tile(0);
