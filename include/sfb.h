@@ -336,8 +336,8 @@ int sfb_prox_rows(sfb_ctx* ctx, float* W, int64_t J, int64_t D, int32_t mode);
  *
  * The rows of a batch are packed: request q is the rows start[q] .. start[q + 1] - 1 of X (any length from zero on) and
  * uses block adapter[q]; a number outside [0, count) means none, the shared matrix alone.  Rows in front of start[0] and
- * from start[requests] on belong to no request: they are not computed, and the outputs' rows there stay as they were (a
- * padded batch).  start and adapter are device arrays, read when the call runs, so that a captured graph serves batches of
+ * from start[requests] on belong to no request (a padded batch): what X and dY hold there does not matter, and the outputs' rows
+ * there stay as they were (they still take their share of the product's time).  start and adapter are device arrays, read when the call runs, so that a captured graph serves batches of
  * other compositions; start must be non-decreasing in [0, T] (other values give unspecified results in the rows they touch,
  * nothing is read or written out of bounds).
  */
@@ -367,6 +367,9 @@ typedef struct {
  * W, fp32 blocks: the fp32 array (w_dtype SFB_F32).  bf16 blocks: a row-major bf16 array [J][D] (w_dtype SFB_BF16), or the
  * fp32 array that is attached to this context with a bf16 working copy or as two planes (w_dtype SFB_F32): the copy or the
  * high plane is read.  bf16 needs J % 8 == 0 and D % 8 == 0, and takes J and D up to 4194304.
+ * The second product takes H (backward: dH) in fp32 or, with bf16 blocks and many rows, as a sum of two bf16 terms that is off by up
+ * to 2^-16 of it: a row in a batch of another size may differ by that and by the order of the sums.  What is written to H, and
+ * what dU and dV are made of, is fp32 throughout.
  * T: up to 16777216.
  *
  * sfb_adapter_backward: the gradients of a loss with dY = d loss / d Y given,
@@ -416,8 +419,9 @@ int sfb_tensor_table_fill(const sfb_tensor* list, int64_t count, void* host);
 int sfb_grad_norm(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, const void* table, float* norm);
 int sfb_clip_grads(sfb_ctx* ctx, const sfb_tensor* list, int64_t count, const void* table, float max_norm, float* norm);
 
-/* 1 while the context's stream is being captured into a HIP graph (the caller then has to keep what the calls work in, the
- * workspace among it, for as long as the graph is replayed), otherwise 0. */
+/* 1 while the context's stream is being captured into a HIP graph, otherwise 0.  What captured calls work in, the workspace among
+ * it, has to stay for as long as the graph is replayed, and is used by one call at a time: replays of graphs of one context, and
+ * its other calls, must not overlap in time. */
 int sfb_capturing(sfb_ctx* ctx);
 /* Static description of a status code. */
 const char* sfb_strerror(int code);

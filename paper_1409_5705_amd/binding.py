@@ -304,7 +304,7 @@ class TensorList:
 
 class Context:
     """One sfb_ctx bound to a device and a stream; owns a torch workspace tensor.  Graphs that captured its calls work in memory
-    that it holds: keep it for as long as they are replayed."""
+    that it holds: keep it for as long as they are replayed, and let no two of them, nor one and a call, run at the same time."""
 
     def __init__(self, device=0, stream=None):
         self._h = ctypes.c_void_p()

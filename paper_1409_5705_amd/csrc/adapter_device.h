@@ -91,8 +91,10 @@ inline int project_factors(int64_t tiles, int pitch, const DeviceInfo& dev)
     return rt;
 }
 
-// Two bf16 terms of a value: its upper half as it is and what is left, rounded (together off by at most 2^-17 of the value, and
-// of its sign); one that is not finite as itself twice.
+// Two bf16 terms of a value: its upper half as it is and what is left, rounded; one that is not finite as itself twice.  Together
+// they are off by at most 2^-16 of the value (what is left is below 2^-7 of it and keeps eight bits; 1 + 2^-8 + 2^-16 is off by
+// that) and both of its sign: where products with them overflow they do so to the same side.  The first term rounded would halve
+// the error and lose that.
 __device__ __forceinline__ void two_terms(float v, uint16_t& first, uint16_t& second)
 {
     const uint32_t bits = __float_as_uint(v);
